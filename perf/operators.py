@@ -1,0 +1,521 @@
+"""The cache operators beside the decode step, as a decoding program uses them.
+
+  window   one token's attention over the first tokens and a sliding window
+  prefill  the same for the chunk of tokens that a prefill appends
+  packed   one token's attention over a cache held in 4 bits: all of it, with
+           the importance S of its tokens, or over a selection
+  write    a prefill hands its K and V over to the 4-bit cache, and a later
+           chunk reads them back
+  evict    a cache made shorter by S: the heaviest tokens stay, in order
+
+Shapes are those of the package's workloads (32 MHA heads, GQA 32/8, 28/4 and
+8/1, head_dim 128; 1K to 131K cached tokens; 1 to 32 sequences, ragged ones
+among them; both 16-bit types).  Inputs are seeded random tensors: keys
+N(0,1), with per-channel LogNormal outlier scales in the 4-bit caches; the
+importance is a LogNormal over the tokens.
+
+A layer's cache is read once per pass; small ones come as several layers, so
+that they come from memory as they do in a model.
+
+The 4-bit format: a row of 128 elements is four groups of 32, each with
+scale = fp16((max - min) * fp32(1/15)) and zero = fp16(min); in fp32,
+code = rint((x - zero) * (1 / scale)) in [0, 15] (0 where scale is 0); a code
+stands for fp16(code * scale + zero), rounded once.  Elements are taken into
+[-65504, 65504].  Codes are 64 bytes a row: each 4-byte word holds eight,
+element 2i in bits 4i..4i+3 and element 2i+1 in bits 16+4i..19+4i.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False                           # True: run() makes the package's calls
+
+D = 128
+RING = 4                              # queries (importance rows) that the passes of one state walk through
+MAX_ROWS = 32 * 8 * 16384             # key rows of a 16-bit cache at most
+MAX_PACKED_ROWS = 4 * 8 * 131072      # of a 4-bit cache
+MAX_PREFILL = 32 * 16384 * 4096       # (query head, token, visible token) triples
+
+
+def _lib():
+    import paper_2602_18750_amd
+    return paper_2602_18750_amd
+
+
+def _case(kind, **kw):
+    c = dict(kind=kind, b=1, hq=32, hkv=8, n=4096, t=1, dtype="bf16", sink=4, window=1024, layers=1, ragged=False,
+             score=False, pick=0.0, keep=0.5, rows="token", packed=False)
+    c.update(kw)
+    return c
+
+
+def listed():
+    return [
+        # one token of a short chat turn, called as a function: latency and launches
+        _case("window", name="window-short", n=1021, window=512),
+        # a ragged serving batch of a 32-head MHA model, two layers, as a marshalled loop
+        _case("window", name="window-ragged-8x4k", b=8, hkv=32, n=4096, dtype="fp16", ragged=True, layers=2),
+        # a full serving batch with a long window, the largest decode pass
+        _case("window", name="window-32x16k", b=32, n=16384, window=4096, sink=128),
+        # a prompt of 16K tokens, the largest prefill
+        _case("prefill", name="prefill-16k", n=16384, t=16384, window=4096),
+        # chunks of a ragged batch of long prompts, 7 heads per KV head
+        _case("prefill", name="prefill-chunk-4x20k", b=4, hq=28, hkv=4, n=20011, t=509, dtype="fp16", window=2048, sink=64,
+              ragged=True),
+        # a 32K decode over the 4-bit caches of eight layers
+        _case("packed", name="packed-32k", n=32768, window=32768, layers=8),
+        # four long documents whose tokens' importance is kept for eviction, the largest 4-bit pass
+        _case("packed", name="packed-score-4x131k", b=4, n=131072, window=131072, score=True),
+        # the tokens that a selection picked, MHA
+        _case("packed", name="packed-picked-2x16k", b=2, hkv=32, n=16384, dtype="fp16", pick=0.10),
+        # a prefill hands a layer's 32K cache over, and a chunk reads it back
+        _case("write", name="packed-write-32k", n=32768),
+        # a full cache gives one token up for the next one (every step of a bounded cache)
+        _case("evict", name="evict-one-of-4k", hkv=32, n=4097, dtype="fp16", keep=1.0),
+        # after a long prefill: half of a 32K cache, four layers
+        _case("evict", name="evict-half-32k", n=32768, sink=4, window=1024, layers=4),
+        # 4-bit caches of a batch, each KV head its own tokens
+        _case("evict", name="evict-packed-4x20k", b=4, hq=28, hkv=4, n=20011, keep=0.4, rows="kvhead", packed=True,
+              window=64, layers=2),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    heads = rng.choice([(32, 8), (32, 8), (32, 8), (32, 32), (28, 4), (16, 8), (8, 1), (40, 8), (64, 8)])
+    kind = rng.choice(["window", "window", "prefill", "prefill", "packed", "packed", "write", "evict", "evict"])
+    c = dict(hq=heads[0], hkv=heads[1], dtype=rng.choice(["bf16", "bf16", "fp16"]), sink=rng.choice([0, 1, 4, 64]),
+             b=rng.choice([1, 1, 2, 3, 5, 8, 16, 32]), n=_log_int(rng, 256, 65536))
+    rows = MAX_PACKED_ROWS // 2 if kind == "packed" else MAX_ROWS // 4
+    while c["b"] > 1 and c["b"] * c["hkv"] * c["n"] > rows:
+        c["b"] //= 2
+    c["n"] = min(c["n"], rows // (c["b"] * c["hkv"]))
+    fit = c["b"] * c["hkv"] * c["n"]
+    c["layers"] = max(1, min(8, (1 << (20 if kind == "packed" else 19)) // fit))
+    if kind == "window":
+        return _case(kind, **dict(c, window=_log_int(rng, 64, 8192), ragged=rng.random() < 0.5))
+    if kind == "prefill":
+        c.update(window=_log_int(rng, 64, 8192), t=min(c["n"], _log_int(rng, 1, 8192)), layers=1)
+        seen = c["hq"] * c["b"] * (min(c["n"], c["window"] + c["sink"]) + 1)
+        c["t"] = max(1, min(c["t"], MAX_PREFILL // 2 // seen))
+        return _case(kind, **dict(c, ragged=rng.random() < 0.5))
+    if kind == "packed":
+        how = rng.choice(["all", "window", "score", "pick"])
+        c["window"] = _log_int(rng, 64, 8192) if how == "window" else c["n"]
+        if how == "pick":
+            c.update(pick=rng.choice([0.05, 0.10, 0.20]), rows=rng.choice(["token", "kvhead"]))
+        elif how == "score":
+            c.update(score=True, rows=rng.choice(["token", "kvhead"]))
+        return _case(kind, **dict(c, ragged=how != "pick" and rng.random() < 0.5))
+    if kind == "write":
+        return _case(kind, **dict(c, layers=1))
+    c.update(keep=rng.choice([1.0, 0.9, 0.75, 0.5, 0.25]), window=rng.choice([0, 32, 128]), rows=rng.choice(["token", "kvhead"]),
+             packed=rng.random() < 0.4)
+    return _case(kind, **c)
+
+
+# ------------------------------------------------------------------ inputs --
+
+def _dt(c):
+    return torch.float16 if c["dtype"] == "fp16" else torch.bfloat16
+
+
+def _keep(c):
+    """Tokens that an eviction keeps: a share, or (1.0) all but one."""
+    k = c["n"] - 1 if c["keep"] == 1.0 else int(c["keep"] * c["n"])
+    return max(1, min(c["n"], c["sink"] + c["window"]), k)
+
+
+def _picks(c):
+    return max(1, int(c["pick"] * c["n"]))
+
+
+def _r(c):
+    return 1 if c["rows"] == "token" else c["hkv"]
+
+
+def _randn(shape, g, dt, scale=None):
+    """N(0,1) in dt, drawn per sequence."""
+    x = torch.empty(shape, dtype=dt, device=g.device)
+    for i in range(shape[0]):
+        y = torch.randn(shape[1:], generator=g, device=g.device)
+        x[i] = y if scale is None else y * scale
+    return x
+
+
+def _inputs(c, seed):
+    """Everything drawn: per layer K and V [B, Hkv, n, D], the queries [RING, layers, B, Hq, t, D], the lengths,
+    importance rows [RING, B, R, n] and (picked) indices."""
+    g = torch.Generator(device="cuda").manual_seed(int(seed))
+    b, hkv, n, dt = c["b"], c["hkv"], c["n"], _dt(c)
+    kv = []
+    for _ in range(c["layers"]):
+        ch = torch.exp(torch.randn((hkv, 1, D), generator=g, device="cuda")) if c["kind"] in ("packed", "write") else None
+        kv.append((_randn((b, hkv, n, D), g, dt, ch), _randn((b, hkv, n, D), g, dt)))
+    ring = 1 if c["kind"] == "prefill" else RING
+    q = torch.randn((ring, c["layers"], b, c["hq"], c["t"], D), generator=g, device="cuda").to(dt)
+    lens = torch.randint(1, n + 1, (b,), generator=g, device="cuda", dtype=torch.int32)
+    lens[0] = n
+    if c["ragged"] and b > 2:
+        lens[-1] = 1
+    s = torch.exp(torch.randn((ring, b, _r(c), n), generator=g, device="cuda"))
+    idx = None
+    if c["pick"]:
+        order = torch.rand((b, _r(c), n), generator=g, device="cuda").argsort(-1)[..., :_picks(c)]
+        idx = torch.sort(order, -1).values.to(torch.int32)
+    return kv, q, lens if c["ragged"] else None, s, idx
+
+
+def _once_to_half(x):
+    """fp16 of 64-bit values, rounded once: through fp32 rounded to odd."""
+    f = x.float()
+    away = f.double().abs() > x.abs()
+    bits = f.view(torch.int32) - away.to(torch.int32)
+    return (bits | (f.double() != x).to(torch.int32)).view(torch.float32).half()
+
+
+def _quantise(x):
+    """Codes [..., 4, 32] and (scale, zero) [..., 4, 2] of 16-bit rows [..., 128]."""
+    g = x.float().clamp(-65504.0, 65504.0).unflatten(-1, (4, 32))
+    lo, hi = g.amin(-1), g.amax(-1)
+    scale, zero = ((hi - lo) * torch.tensor(1.0 / 15.0, dtype=torch.float32)).half(), lo.half()
+    s32 = scale.float()
+    inv = torch.where(s32 > 0, 1.0 / s32, torch.zeros_like(s32))
+    code = torch.round((g - zero.float()[..., None]) * inv[..., None]).clamp(0, 15)
+    return code.to(torch.uint8), torch.stack((scale, zero), -1)
+
+
+def _values(code, par):
+    """fp16 rows [..., 128] that codes [..., 4, 32] and (scale, zero) stand for."""
+    p = par.double()
+    return _once_to_half(code.double() * p[..., 0:1] + p[..., 1:2]).flatten(-2)
+
+
+def _to_bytes(code):
+    """[..., 4, 32] codes -> [..., 64] bytes (the order of the format)."""
+    w = code.flatten(-2).unflatten(-1, (16, 2, 2, 2))          # word, byte of a half, low / high nibble, half
+    w = w[..., 0, :] | (w[..., 1, :] << 4)                     # word, byte, half
+    return w.transpose(-1, -2).flatten(-3).contiguous()
+
+
+def _from_bytes(by):
+    w = by.unflatten(-1, (16, 2, 2)).transpose(-1, -2)         # word, byte of a half, half
+    return torch.stack((w & 15, w >> 4), -2).flatten(-4).unflatten(-1, (4, 32))
+
+
+def _pack_rows(x):
+    """Bytes and (scale, zero) of [B, Hkv, n, D], a sequence at a time."""
+    by = torch.empty(x.shape[:3] + (64,), dtype=torch.uint8, device=x.device)
+    par = torch.empty(x.shape[:3] + (4, 2), dtype=torch.float16, device=x.device)
+    for b in range(x.shape[0]):
+        code, par[b] = _quantise(x[b])
+        by[b] = _to_bytes(code)
+    return by, par
+
+
+def prepare(case, seed):
+    c = dict(case)
+    kv, q, lens, s, idx = _inputs(c, seed)
+    b, hkv, n, r = c["b"], c["hkv"], c["n"], _r(c)
+    st = dict(c=c, q=q, lens=lens, ring=s, idx=idx, t=0, kv=kv)
+    if c["kind"] == "packed" or c["packed"]:
+        st["cache"] = [_pack_rows(k) + _pack_rows(v) for k, v in kv]
+        del st["kv"], kv
+    elif c["kind"] == "write":
+        st["cache"] = [(torch.zeros((b, hkv, n, 64), dtype=torch.uint8, device="cuda"),
+                        torch.zeros((b, hkv, n, 4, 2), dtype=torch.float16, device="cuda")) * 2]
+    st["s"] = []
+    for i in range(c["layers"] if c["kind"] == "evict" or c["score"] else 0):
+        row = torch.zeros((b, r, (n + 3) // 4 * 4), device="cuda")[:, :, :n]
+        row.copy_(s[i % RING])
+        st["s"].append(row)
+    if c["kind"] == "evict":
+        st["pos"] = [torch.arange(n, dtype=torch.int32, device="cuda").expand(b, r, n).contiguous() for _ in range(c["layers"])]
+    if own:
+        lib = _lib()
+        st["ptrs"] = [[q[t, i].data_ptr() for i in range(c["layers"])] for t in range(q.shape[0])]
+        if "cache" in st:
+            st["caches"] = [lib.PackedCache(*p) for p in st["cache"]]
+        if c["kind"] == "window" and c["layers"] > 1:
+            st["calls"] = [lib.WindowAttnCall(q[0, i, :, :, 0], k, v, window=c["window"], n_sink=c["sink"], lens=lens)
+                           for i, (k, v) in enumerate(kv)]
+        if c["kind"] == "packed":
+            st["calls"] = [lib.PackedAttnCall(q[0, i, :, :, 0], cache, window=None if c["window"] >= n else c["window"],
+                                              n_sink=c["sink"], lens=lens, idx=idx, granularity=c["rows"],
+                                              s=st["s"][i] if c["score"] else None) for i, cache in enumerate(st["caches"])]
+    return st
+
+
+# -------------------------------------------------------- the operators --
+
+def _softmax(x):
+    """Over the last axis; rows of nothing but -inf weigh 0."""
+    m = x.amax(-1, keepdim=True)
+    e = torch.exp(x - torch.where(m == -math.inf, torch.zeros_like(m), m))
+    total = e.sum(-1, keepdim=True)
+    return e / torch.where(total == 0, torch.ones_like(total), total)
+
+
+def _visible(c, n):
+    """Indices that the last of n tokens sees."""
+    j = torch.arange(n, device="cuda")
+    return j[(j < c["sink"]) | (j >= n - c["window"])]
+
+
+def _len(lens, b, n):
+    return n if lens is None else int(lens[b])
+
+
+def _one_token(c, q, k, v, out):
+    """q [Hq, D], k and v [Hkv, m, D] in 32 bits -> weights [Hkv, G, m]; writes out [Hq, D]."""
+    g = c["hq"] // c["hkv"]
+    w = _softmax(torch.matmul(q.view(c["hkv"], g, D), k.transpose(1, 2).contiguous()) / math.sqrt(D))
+    out.copy_(torch.matmul(w, v).reshape(c["hq"], D))
+    return w
+
+
+def _chunk(c, q, k, v, n, out):
+    """q and out [Hq, T, D], the last T of n tokens; k, v [Hkv, >= n, D]; 256 tokens at a time."""
+    g, t_all = c["hq"] // c["hkv"], q.shape[1]
+    for t0 in range(0, t_all, 256):
+        t1 = min(t_all, t0 + 256)
+        p = torch.arange(n - t_all + t0, n - t_all + t1, device="cuda")
+        lo, hi = max(0, n - t_all + t0 - c["window"] + 1), max(0, n - t_all + t1)
+        j = torch.cat((torch.arange(0, min(c["sink"], lo, hi), device="cuda"), torch.arange(min(lo, hi), hi, device="cuda")))
+        if j.numel() == 0:
+            out[:, t0:t1] = 0
+            continue
+        d = p[:, None] - j[None, :]
+        seen = (d >= 0) & ((j[None, :] < c["sink"]) | (d < c["window"]))
+        kk, vv = k[:, j].float().transpose(1, 2).contiguous(), v[:, j].float()
+        qq = q[:, t0:t1].float().reshape(c["hkv"], g * (t1 - t0), D)
+        x = (torch.matmul(qq, kk) / math.sqrt(D)).view(c["hkv"], g, t1 - t0, -1)
+        w = _softmax(x.masked_fill(~seen, -math.inf))
+        out[:, t0:t1] = torch.matmul(w.view(c["hkv"], g * (t1 - t0), -1), vv).view(c["hq"], t1 - t0, D).to(out.dtype)
+
+
+def _plain(st, t):
+    c, lens = st["c"], st["lens"]
+    b, hq, n = c["b"], c["hq"], c["n"]
+    if c["kind"] == "window":
+        outs = []
+        for i, (k, v) in enumerate(st["kv"]):
+            out = torch.zeros((b, hq, D), device="cuda")
+            for s in range(b):
+                j = _visible(c, _len(lens, s, n))
+                if j.numel():
+                    _one_token(c, st["q"][t, i, s, :, 0].float(), k[s][:, j].float(), v[s][:, j].float(), out[s])
+            outs.append(out)
+        return dict(out=outs)
+    if c["kind"] == "prefill":
+        out = torch.zeros((b, hq, c["t"], D), dtype=_dt(c), device="cuda")
+        for s in range(b):
+            _chunk(c, st["q"][0, 0, s], st["kv"][0][0][s], st["kv"][0][1][s], _len(lens, s, n), out[s])
+        return dict(out=out)
+    if c["kind"] == "packed":
+        outs = []
+        for i, (kb, kp, vb, vp) in enumerate(st["cache"]):
+            out = torch.zeros((b, hq, D), device="cuda")
+            for s in range(b):
+                if st["idx"] is None:
+                    j = _visible(c, _len(lens, s, n))
+                    if not j.numel():
+                        continue
+                    k, v = (_values(_from_bytes(x[s][:, j]), p[s][:, j]).float() for x, p in ((kb, kp), (vb, vp)))
+                else:
+                    j = st["idx"][s].long()
+                    h = torch.arange(c["hkv"], device="cuda")[:, None]
+                    k, v = (_values(_from_bytes(x[s][h, j]), p[s][h, j]).float() for x, p in ((kb, kp), (vb, vp)))
+                w = _one_token(c, st["q"][t, i, s, :, 0].float(), k, v, out[s])
+                if c["score"]:
+                    w = w.sum(1)
+                    st["s"][i][s][:, j] += w if _r(c) > 1 else w.sum(0, keepdim=True)
+            outs.append(out)
+        return dict(out=outs, s=st["s"])
+    if c["kind"] == "write":
+        k, v = st["kv"][0]
+        got = []
+        for x, by, par in ((k, *st["cache"][0][:2]), (v, *st["cache"][0][2:])):
+            y = torch.empty_like(x)
+            for s in range(b):
+                code, par[s] = _quantise(x[s])
+                by[s] = _to_bytes(code)
+                y[s] = _values(_from_bytes(by[s]), par[s]).to(x.dtype)
+            got.append(y)
+        return dict(k=got[0], v=got[1])
+    keep, idxs, held = _keep(c), [], []
+    for i, (s, pos) in enumerate(zip(st["s"], st["pos"])):
+        s.copy_(st["ring"][(t + i) % RING])
+        x = s.clone()
+        x[:, :, :c["sink"]] = math.inf
+        if c["window"]:
+            x[:, :, max(0, n - c["window"]):] = math.inf
+        idx = torch.sort(torch.sort(x, dim=-1, descending=True, stable=True).indices[..., :keep], -1).values
+        s[:, :, :keep] = s.gather(-1, idx)
+        s[:, :, keep:] = 0
+        pos[:, :, :keep] = pos.gather(-1, idx)
+        buffers = st["cache"][i] if c["packed"] else st["kv"][i]
+        for buf in buffers:
+            flat = buf.flatten(3)
+            j = idx[:, :, :, None].expand(b, c["hkv"], keep, flat.shape[3])
+            flat[:, :, :keep] = flat.gather(2, j)
+        idxs.append(idx.to(torch.int32))
+        held.append([buf[:, :, :keep] for buf in buffers])
+    return dict(idx=idxs, s=st["s"], pos=[p[:, :, :keep] for p in st["pos"]], kv=held)
+
+
+def run(st):
+    c, t = st["c"], st["t"]
+    st["t"] = (t + 1) % st["q"].shape[0]
+    if not own:
+        return _plain(st, t)
+    lib = _lib()
+    if "calls" in st:
+        for call, p in zip(st["calls"], st["ptrs"][t]):
+            call(p)
+        outs = [call.out for call in st["calls"]]
+        return dict(out=outs, s=st["s"]) if c["kind"] == "packed" else dict(out=outs)
+    if c["kind"] == "window":
+        k, v = st["kv"][0]
+        return dict(out=[lib.hill_window_attn(st["q"][t, 0, :, :, 0], k, v, window=c["window"], n_sink=c["sink"],
+                                              lens=st["lens"])])
+    if c["kind"] == "prefill":
+        k, v = st["kv"][0]
+        return dict(out=lib.hill_window_prefill(st["q"][0, 0], k, v, window=c["window"], n_sink=c["sink"],
+                                                lens=st["lens"]))
+    if c["kind"] == "write":
+        k, v = st["kv"][0]
+        lib.pack_kv(k, v, st["caches"][0])
+        k, v = lib.unpack_kv(st["caches"][0], dtype=_dt(c))
+        return dict(k=k, v=v)
+    keep, idxs, held = _keep(c), [], []
+    for i, (s, pos) in enumerate(zip(st["s"], st["pos"])):
+        s.copy_(st["ring"][(t + i) % RING])
+        held_in = dict(cache=st["caches"][i]) if c["packed"] else dict(k=st["kv"][i][0], v=st["kv"][i][1])
+        idxs.append(lib.hill_evict(s, keep, pos=pos, granularity=c["rows"], n_sink=c["sink"], n_recent=c["window"], **held_in))
+        held.append([buf[:, :, :keep] for buf in (st["cache"][i] if c["packed"] else st["kv"][i])])
+    return dict(idx=idxs, s=st["s"], pos=[p[:, :, :keep] for p in st["pos"]], kv=held)
+
+
+def _seen(c, n, t):
+    """(query token, visible token) pairs of the last t of n tokens."""
+    return sum(min(p + 1, min(c["sink"], max(0, p + 1 - c["window"])) + c["window"]) for p in range(max(0, n - t), n))
+
+
+def work(case):
+    c = case
+    b, hq, hkv, n, layers, r = c["b"], c["hq"], c["hkv"], c["n"], c["layers"], _r(c)
+    rows = b * hkv * n
+    mean = 0.5 if c["ragged"] and b > 1 else 1.0      # drawn lengths: the first whole, the others uniform
+    fill = (1 + (b - 1) * mean) / b
+    if c["kind"] == "write":
+        return dict(bytes=rows * 2 * (256 + 80 + 80 + 256), flops=rows * 2 * D * 6)
+    if c["kind"] == "evict":
+        keep = _keep(c)
+        row = 160 if c["packed"] else 512
+        moved = keep // 2 if c["keep"] == 1.0 else keep       # one gap, anywhere: the rows before it stay
+        return dict(bytes=layers * (b * hkv * moved * row * 2 + b * r * (4 * n + 4 * n + 12 * keep)), flops=layers * b * r * n)
+    if c["kind"] == "prefill":
+        pairs = int(b * fill * _seen(c, n, c["t"]))
+        keys = b * fill * min(n, c["t"] + c["window"] + c["sink"])
+        return dict(bytes=int(hkv * keys * 512 + 2 * b * hq * c["t"] * 256), flops=4 * D * hq * pairs)
+    seen = _picks(c) if c["pick"] else min(int(n * fill), c["sink"] + c["window"])
+    by = b * hkv * seen * (512 if c["kind"] == "window" else 160) + b * hq * 6 * D + (4 * b * r * seen if c["pick"] else 0)
+    if c["score"]:
+        by += 8 * b * r * seen
+    return dict(bytes=layers * by, flops=layers * 4 * D * b * hq * seen)
+
+
+# ------------------------------------------------- the same, in 64 bits --
+
+def _quantised64(x):
+    """The fp16 values that the 4-bit cache holds for 16-bit rows x, in 64 bits (the format's fp32 steps by rounding
+    64-bit results to fp32, which is what one fp32 operation gives)."""
+    once = lambda y: y.float().double()
+    a = torch.minimum(torch.maximum(x.double(), x.new_tensor(-65504.0).double()), x.new_tensor(65504.0).double())
+    a = a.reshape(x.shape[:-1] + (4, 32))
+    lo, hi = a.min(-1, keepdim=True).values, a.max(-1, keepdim=True).values
+    scale = _half64(once(once(hi - lo) * float(np.float32(1.0) / np.float32(15.0))))
+    zero = _half64(lo)
+    inv = torch.where(scale > 0, once(1.0 / scale.clamp_min(2.0 ** -24)), torch.zeros_like(scale))
+    code = torch.round(once(once(a - zero) * inv)).clamp(0, 15)
+    return _half64(code * scale + zero).reshape(x.shape)
+
+
+def _half64(v):
+    """64-bit values rounded to the nearest fp16 value, ties to even."""
+    step = torch.exp2((torch.frexp(v).exponent.double() - 11).clamp_min(-24))
+    return torch.round(v / step) * step
+
+
+def _attend64(q, k, v, mask):
+    """q [G, T, D], k and v [m, D], mask [T, m] of one KV head in 64 bits -> out [G, T, D], weights [G, T, m]."""
+    x = (q.reshape(-1, D) @ k.T).view(q.shape[0], q.shape[1], -1) * D ** -0.5
+    e = torch.where(mask, torch.exp(x - x.masked_fill(~mask, -1e300).amax(-1, keepdim=True)), torch.zeros_like(x))
+    w = e / e.sum(-1, keepdim=True).clamp_min(1e-300)
+    return (w.view(-1, w.shape[-1]) @ v).view(q.shape), w
+
+
+def exact(case, seed):
+    c = dict(case)
+    kv, q, lens, ring, idx = _inputs(c, seed)
+    b, hq, hkv, n, r = c["b"], c["hq"], c["hkv"], c["n"], _r(c)
+    g = hq // hkv
+    if c["kind"] == "write":
+        return dict(k=_quantised64(kv[0][0]).to(_dt(c)).double(), v=_quantised64(kv[0][1]).to(_dt(c)).double())
+    if c["kind"] == "evict":
+        keep = _keep(c)
+        got = dict(idx=[], s=[], pos=[], kv=[])
+        for i in range(c["layers"]):
+            s = ring[i % RING].double()
+            j = torch.arange(n, device="cuda").expand_as(s)
+            pinned = (j < c["sink"]) | (j >= n - c["window"])
+            rank = torch.sort(torch.where(pinned, torch.full_like(s, math.inf), s), dim=-1, descending=True, stable=True).indices
+            stays = torch.zeros_like(pinned).scatter_(-1, rank[..., :keep], True)
+            picked = j[stays].view(b, r, keep)
+            rest = torch.zeros((b, r, n - keep), dtype=torch.float64, device="cuda")
+            got["idx"].append(picked.to(torch.int32))
+            got["s"].append(torch.cat((s[stays].view(b, r, keep), rest), -1))
+            got["pos"].append(picked.to(torch.int32))
+            if c["packed"]:
+                got["kv"].append([None] * 4)
+                continue
+            stays = stays.expand(b, hkv, n) if r == 1 else stays
+            got["kv"].append([x[stays].view(b, hkv, keep, D).double() for x in kv[i]])
+        return got
+    if c["kind"] == "prefill" and b * hq * c["t"] > 4 << 20:
+        return None
+    outs, rows = [], []
+    for i, (k, v) in enumerate(kv):
+        held = _quantised64 if c["kind"] == "packed" else torch.Tensor.double
+        out = torch.zeros((b, hq, c["t"], D), dtype=torch.float64, device="cuda")
+        s = ring[i % RING].double() if c["score"] else None
+        for sb in range(b):
+            m = n if lens is None else int(lens[sb])
+            for h in range(hkv):
+                for t0 in range(0, c["t"], 128):
+                    qq = q[0, i, sb, h * g:(h + 1) * g, t0:t0 + 128].double()
+                    p = m - c["t"] + t0 + torch.arange(qq.shape[1], device="cuda")[:, None]
+                    lo = max(0, m - c["t"] + t0 - c["window"])
+                    j = torch.arange(m, device="cuda")[None, :]
+                    if c["pick"]:
+                        j = idx[sb, h if r > 1 else 0].long()[None, :]
+                        mask = torch.ones((1, j.shape[1]), dtype=torch.bool, device="cuda")
+                    else:
+                        j = j[(j < c["sink"]) | ((j >= lo) & (j <= int(p[-1])))][None, :]
+                        mask = (j <= p) & ((j < c["sink"]) | (j > p - c["window"]))
+                    if not j.numel():
+                        continue
+                    o, w = _attend64(qq, held(k[sb, h, j[0]]), held(v[sb, h, j[0]]), mask)
+                    out[sb, h * g:(h + 1) * g, t0:t0 + 128] = o
+                    if c["score"]:
+                        s[sb, h if r > 1 else 0, j[0]] += w.sum((0, 1))
+        outs.append(out[:, :, 0] if c["kind"] != "prefill" else out)
+        rows += [s] if c["score"] else []
+    if c["kind"] == "prefill":
+        return dict(out=outs[0])
+    return dict(out=outs, s=rows) if c["kind"] == "packed" else dict(out=outs)
