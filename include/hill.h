@@ -67,7 +67,7 @@
 extern "C" {
 #endif
 
-#define HILL_ABI_VERSION 6
+#define HILL_ABI_VERSION 7
 
 /* The library exports these entry points only (built with hidden visibility). */
 #define HILL_API __attribute__((visibility("default")))
@@ -311,6 +311,113 @@ HILL_API hill_status hill_step_sketch(const hill_desc* d, const void* q, const v
                              const int8_t* k8, const int8_t* k_exp, int64_t cap, int32_t bits, float* s,
                              uint32_t* state, uint32_t flags, int32_t k_sel, int32_t* idx_out, float* out,
                              void* ws, size_t ws_bytes, void* stream, const hill_step_events* ev);
+
+/* Attention over the first tokens and a sliding window: the part of a cache
+ * that selections pin (n_sink, n_recent), attended by itself, without scores or
+ * a selection.  A query at position p of its sequence sees token j when
+ *     j <= p  and  (j < n_sink  or  p - j < n_recent);
+ * a query that sees nothing (an empty sequence, or n_sink = n_recent = 0) gets
+ * zeros.  n_recent >= n_tokens attends to everything.  Tokens that no query of
+ * the call sees are not read; whatever their rows hold has no effect.
+ *
+ * lens: NULL, or device int32 [B], 4-byte aligned: the tokens of each sequence,
+ * taken into [0, n_tokens] on the device (n_tokens is then the longest
+ * possible); otherwise every sequence has n_tokens.  The query is the last token
+ * of its sequence (prefill: the last n_new ones).
+ *
+ * Workspace bytes of hill_window_attn (n_new = 0) or hill_window_prefill (its
+ * n_new); they depend on the shape, n_sink and n_recent, and may be 0. */
+HILL_API hill_status hill_window_workspace_bytes(const hill_desc* d, int32_t n_new, size_t* bytes);
+
+/* One token per sequence: q [B, Hq, D], out fp32 [B, Hq, D] as in
+ * hill_gather_attn. */
+HILL_API hill_status hill_window_attn(const hill_desc* d, const void* q, const void* k, const void* v, const int32_t* lens,
+                             float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The last n_new tokens of every sequence, whose K and V rows the cache
+ * already holds (a prefill, or one chunk of it).  q and out: [B, Hq, n_new, D] in
+ * d's dtype, q with d's strides and q_stride_t between tokens, out with strides of its own, all
+ * multiples of 8 elements (a [B, n_new, Hq, D] tensor has stride_t = Hq * D, stride_h = D);
+ * both 16-byte aligned, out disjoint from the inputs.  Query i has position lens[b] - n_new + i;
+ * where that is negative (a sequence shorter than the chunk, padded in front) its output is
+ * zero.  The softmax weights and the output are rounded to d's dtype, sums are fp32. */
+typedef struct hill_prefill_desc {
+    uint32_t struct_size;     /* sizeof(hill_prefill_desc) */
+    int32_t n_new;            /* 1 <= n_new <= n_tokens */
+    int64_t q_stride_t;
+    int64_t o_stride_b, o_stride_h, o_stride_t;
+} hill_prefill_desc;
+
+HILL_API hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, const void* q, const void* k,
+                                const void* v, const int32_t* lens, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Cache held in 4 bits.  A row of 128 elements is four groups of 32, each with
+ *     scale = fp16((max - min) * (1/15 in fp32)),  zero = fp16(min);
+ *     code  = rint((x - zero) * (1 / scale)) in [0, 15], in fp32 (0 where scale is 0);
+ * a code stands for fp16(code * scale + zero), rounded once.  Elements beyond
+ * fp16's largest are taken as that.  160 bytes per token and KV head hold K and V,
+ * instead of 512.
+ *
+ * Layouts, all contiguous and 16-byte aligned: k_codes, v_codes [B, Hkv, cap, 64]
+ * bytes (each little-endian 4-byte word holds elements 8w..8w+7: element 2i in bits
+ * 4i..4i+3, element 2i+1 in bits 16+4i..19+4i); k_params, v_params
+ * [B, Hkv, cap, 4] pairs of fp16 (scale, zero).  B, Hkv and the 16-bit dtype
+ * are the descriptor's. */
+typedef struct hill_packed {
+    uint32_t struct_size;     /* sizeof(hill_packed) */
+    int32_t cap;              /* rows per (b, g), >= 1 */
+    void* k_codes;
+    void* k_params;
+    void* v_codes;
+    void* v_params;
+} hill_packed;
+
+/* Writes n_tokens rows of k and v (d's dtype and strides) per (b, g): row i of
+ * sequence b becomes cache row at[b] + i (at: device int32 [B], 4-byte
+ * aligned) or at0 + i (at NULL).  Rows that would land outside [0, cap) are not
+ * written.  No score or q field of d is used. */
+HILL_API hill_status hill_pack_kv(const hill_desc* d, const hill_packed* p, const void* k, const void* v, const int32_t* at,
+                         int32_t at0, void* stream);
+
+/* Reads cache rows [token_begin, token_end) back as 16-bit rows: row
+ * token_begin + i of (b, g) to row i of k and v (d's dtype and strides, n_tokens >=
+ * token_end - token_begin rows); fp16 holds the values exactly, bf16 rounds them. */
+HILL_API hill_status hill_unpack_kv(const hill_desc* d, const hill_packed* p, int32_t token_begin, int32_t token_end, void* k,
+                           void* v, void* stream);
+
+/* Workspace bytes of hill_packed_attn; k_sel 0 without idx, with_s nonzero with s. */
+HILL_API hill_status hill_packed_workspace_bytes(const hill_desc* d, int32_t k_sel, int32_t with_s, size_t* bytes);
+
+/* One token's attention over a cache held in 4 bits; q [B, Hq, D], out fp32
+ * [B, Hq, D], n_tokens <= cap; d's k and v strides are checked but not used.
+ * idx NULL: over what hill_window_attn would see (n_sink, n_recent, lens).
+ * idx [B, R, k_sel] int32: over those rows (as hill_gather_attn; n_sink, n_recent
+ * are not used, lens and s must be NULL).
+ * s: NULL, or the cumulative importance: S[b,r,j] += sum of the weights of row r's
+ * heads for every token they see, as hill_score adds them (the weights here are those of the visible
+ * tokens); other entries are not touched. */
+HILL_API hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, const void* q, const int32_t* lens,
+                             const int32_t* idx, int32_t k_sel, float* s, float* out, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/* Eviction by accumulated attention weight: makes every row's cache k_keep
+ * tokens long.  idx_out [B, R, k_keep] int32 receives hill_topk's selection of S
+ * (n_sink, n_recent pinned, ties to the lower index); then, in place, row i of
+ * the cache becomes what row idx_out[b, r, i] was, for i < k_keep, in:
+ *   k, v     16-bit rows (d's strides, rows that do not overlap), or
+ *   p        a packed cache (n_tokens <= cap), or neither;
+ *   s        the importance, whose entries [k_keep, n_tokens) become 0, as hill_score
+ *            wants them for tokens to come;
+ *   pos      NULL, or int32 with S's strides, such as the tokens' positions.
+ * All KV heads of a sequence keep the same tokens (HILL_SEL_TOKEN) or each its own
+ * (HILL_SEL_KVHEAD).  Other rows of k, v, p and pos from k_keep on are left as they
+ * were.  The order of tokens stays, so the first n_sink and the last tokens are
+ * where selections, windows and later evictions look for them.  A key sketch or
+ * pool state of the cache is not moved: rewrite it (hill_sketch_keys), or clear it;
+ * a streamed selection goes on with a zeroed state. */
+HILL_API hill_status hill_evict_workspace_bytes(const hill_desc* d, int32_t k_keep, size_t* bytes);
+HILL_API hill_status hill_evict(const hill_desc* d, float* s, int32_t k_keep, int32_t* idx_out, void* k, void* v,
+                       const hill_packed* p, int32_t* pos, void* ws, size_t ws_bytes, void* stream);
 
 /* Bidirectional KV Cache Pools (Sec. 4.2, HKM / BKP): the per-token hit-rate
  * table and the hot/cold pool policy, run once after each decoding step (the

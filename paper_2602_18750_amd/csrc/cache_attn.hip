@@ -1,0 +1,432 @@
+// One token's dense attention over a cache: over the first tokens and a
+// sliding window of 16-bit rows, over the same or all rows of a cache held in
+// 4 bits, or over a list of the latter's rows; optionally with the logits kept
+// for the importance S.
+//
+//   x_i = s2 * q.K_j(i),  m = max x,  l = sum 2^(x - m),  out = sum 2^(x - m) V / l
+//
+//  cache_attn   one (sequence, KV head, 16 query heads, share of the visible
+//               positions) per workgroup of four waves, one pass with running
+//               m and l
+//  cache_merge  the shares of a head joined, and S += the weights
+//
+// The bound is memory: 512 B (16-bit) or 160 B (4-bit) per token and KV head
+// against 16 heads' products on the matrix cores.  A wave takes 32 tokens at a time,
+// without barriers: K rows come in the operand's layout (lane: one token,
+// 16-byte pieces) and give x^T (tokens x heads), whose lanes hold exactly what
+// the second product's weights operand needs; V rows go through a private 9
+// KiB of LDS and come back transposed.  The rows of the next 32 tokens are
+// requested before the weights of these are formed.  Products are exact in the matrix
+// cores' fp32 sums: the weights are split into 16-bit terms (split_weights), a
+// bf16 query over fp16 values is scaled by a power of two into fp16's range
+// (elements below 2^-29 of its largest lose bits).
+#include "mfma_device.h"
+
+namespace hill {
+
+namespace {
+
+constexpr int kTile = 32;        // tokens per wave and step
+constexpr int kVRow = 144;       // 16-bit elements per V row in LDS: 288 bytes, so that the rows of a transposing
+                                 // read lie in different banks
+constexpr int kHeads = 16;       // query heads per workgroup
+
+enum Rows : int { kRowsF16 = 0, kRowsBf16 = 1, kRowsPacked = 2 };
+
+// What a lane holds of a tile before it is used.
+template <int KT>
+struct TileRegs {
+    uint4 k[KT == kRowsPacked ? 2 : 8];
+    uint4 v[KT == kRowsPacked ? 2 : 8];
+    uint32_t kp[2], vp[2];       // packed: (scale, zero) of the codes above
+};
+
+// Tokens are taken into [0, n), so that a bad list entry reads a valid row.
+template <int KT, bool IDX>
+__device__ __forceinline__ void load_tile(const CacheAttnArgs& a, int b, int g, const Visible& vis, int i0, int tok,
+                                          TileRegs<KT>& t)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, qd = lane >> 4;
+    auto token = [&](int i) {   // of position i0 + i, the last one repeated
+        if constexpr (IDX) return __shfl(tok, i, 64);
+        return vis.token(min(i0 + i, vis.nv - 1));
+    };
+    if constexpr (KT == kRowsPacked) {
+        const int64_t row0 = ((int64_t)b * a.Hkv + g) * a.cap;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t row = row0 + token(16 * u + c);
+            t.k[u] = *reinterpret_cast<const uint4*>(a.kc + row * 64 + qd * 16);
+            t.kp[u] = a.kp[row * 4 + qd];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t row = row0 + token(16 * u + (lane >> 2));
+            t.v[u] = *reinterpret_cast<const uint4*>(a.vc + row * 64 + (lane & 3) * 16);
+            t.vp[u] = a.vp[row * 4 + (lane & 3)];
+        }
+    } else {
+        const uint16_t* kb = a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh + qd * 8;
+        const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh + c * 8;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint16_t* r = kb + (uint64_t)(uint32_t)token(16 * u + c) * (uint32_t)a.k_sn;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.k[4 * u + i] = *reinterpret_cast<const uint4*>(r + 32 * i);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            t.v[u] = *reinterpret_cast<const uint4*>(vb + (uint64_t)(uint32_t)token(4 * u + qd) * (uint32_t)a.v_sn);
+    }
+}
+
+// The V rows of a tile into LDS as 16-bit rows.
+template <int KT>
+__device__ __forceinline__ void stage_values(const TileRegs<KT>& t, uint16_t* vl)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, qd = lane >> 4;
+    if constexpr (KT == kRowsPacked) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            half2_t scale, zero;
+            group_params(t.vp[u], scale, zero);
+            uint4* to = reinterpret_cast<uint4*>(vl + (16 * u + (lane >> 2)) * kVRow + (lane & 3) * 32);
+            to[0] = decode8(t.v[u].x, scale, zero);
+            to[1] = decode8(t.v[u].y, scale, zero);
+            to[2] = decode8(t.v[u].z, scale, zero);
+            to[3] = decode8(t.v[u].w, scale, zero);
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) *reinterpret_cast<uint4*>(vl + (4 * u + qd) * kVRow + c * 8) = t.v[u];
+    }
+}
+
+// x^T of the tile: lane (c, qd) gets tokens 16 u + 4 qd + r of head c.
+template <int KT>
+__device__ __forceinline__ void tile_logits(const TileRegs<KT>& t, const uint4 (&qf)[4], f32x4_v (&x)[2])
+{
+    constexpr int DT = KT == kRowsBf16 ? 1 : 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        x[u] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (KT == kRowsPacked) {
+            half2_t scale, zero;
+            group_params(t.kp[u], scale, zero);
+            const uint32_t w[4] = {t.k[u].x, t.k[u].y, t.k[u].z, t.k[u].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[u] = mfma16<DT>(decode8(w[i], scale, zero), qf[i], x[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[u] = mfma16<DT>(t.k[4 * u + i], qf[i], x[u]);
+        }
+    }
+}
+
+// A query row (lane's 8-element pieces) as fp16: bf16 elements times 2^-e with
+// the row's largest in [2^14, 2^15); returns 2^e.
+__device__ __forceinline__ float bf16_query_to_half(uint4 (&qf)[4])
+{
+    float x[32], m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            widen2<1>(w[j], x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
+            m = fmaxf(m, fmaxf(fabsf(x[8 * i + 2 * j]), fabsf(x[8 * i + 2 * j + 1])));
+        }
+    }
+    m = max_x16_x32(m);
+    int e = 0;
+    if (m > 0.0f && m < INFINITY) {
+        frexpf(m, &e);
+        e -= 15;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const half2_t h = {(_Float16)ldexpf(x[8 * i + 2 * j], -e), (_Float16)ldexpf(x[8 * i + 2 * j + 1], -e)};
+            w[j] = __builtin_bit_cast(uint32_t, h);
+        }
+        qf[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return ldexpf(1.0f, e);
+}
+
+template <int KT, bool IDX, bool LOG>
+__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a)
+{
+    constexpr int DT = KT == kRowsBf16 ? 1 : 0;
+    constexpr int kTerms = kWeightTerms<DT>;
+    __shared__ __attribute__((aligned(16))) uint16_t vlds[4 * kTile * kVRow];   // then the waves' outputs
+    __shared__ float2 ml[4][kHeads];
+    __shared__ float inv_l[kHeads];
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, qd = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int split = blockIdx.x % a.nsplit;
+    int y = blockIdx.x / a.nsplit;
+    const int ht = y % a.head_tiles;
+    y /= a.head_tiles;
+    const int g = y % a.Hkv, b = y / a.Hkv;
+    const int h0 = ht * kHeads;                        // first head of the group
+    const int h = g * a.G + min(h0 + c, a.G - 1);      // heads past the group repeat its last
+    Visible vis;
+    const int32_t* idx = nullptr;
+    if constexpr (IDX) {
+        idx = a.idx + ((int64_t)b * a.R + (a.R > 1 ? g : 0)) * a.ksel;
+        vis.ns = vis.nv = a.ksel;
+        vis.gap = 0;
+    } else {
+        vis = visible(seq_len(a.lens, b, a.n), a.sink, a.window);
+    }
+    const int tiles = (vis.nv + kTile - 1) / kTile, per = (tiles + a.nsplit - 1) / a.nsplit;
+    const int t1 = min(tiles, (split + 1) * per);
+    int t = split * per + w;
+
+    uint4 qf[4];
+    float s2 = a.s2;
+    {
+        const uint16_t* qr = a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            qf[i] = *reinterpret_cast<const uint4*>(qr + (KT == kRowsPacked ? 32 * qd + 8 * i : 32 * i + 8 * qd));
+        if constexpr (KT == kRowsPacked)
+            if (a.q_bf16) s2 *= bf16_query_to_half(qf);
+    }
+
+    uint16_t* vl = vlds + w * kTile * kVRow;
+    const uint16_t* vr = vl + (4 * qd + (c >> 2)) * kVRow + 4 * (c & 3);
+    f32x4_v o[8];
+#pragma unroll
+    for (int d = 0; d < 8; ++d) o[d] = f32x4_v{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -INFINITY, l = 0.0f;
+
+    // tokens of a list tile: lane i (and i + 32) holds that of position i; loaded a tile ahead of its rows
+    auto list_tokens = [&](int tile) {
+        int tok = 0;
+        if constexpr (IDX) tok = min(max(idx[min(tile * kTile + (lane & 31), vis.nv - 1)], 0), a.n - 1);
+        return tok;
+    };
+    TileRegs<KT> regs;
+    int tok = 0;
+    if (t < t1) {
+        load_tile<KT, IDX>(a, b, g, vis, t * kTile, list_tokens(t), regs);
+        tok = list_tokens(min(t + 4, t1 - 1));
+    }
+    for (; t < t1; t += 4) {
+        f32x4_v x[2];
+        stage_values<KT>(regs, vl);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // other lanes read what this one wrote
+        tile_logits<KT>(regs, qf, x);
+        if (t + 4 < t1) {
+            load_tile<KT, IDX>(a, b, g, vis, (t + 4) * kTile, tok, regs);
+            tok = list_tokens(min(t + 8, t1 - 1));
+        }
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = x[e >> 2][e & 3] * s2;
+        const int i0 = t * kTile + 4 * qd;             // this lane's positions: i0 + r and i0 + 16 + r
+        if ((t + 1) * kTile > vis.nv) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i0 + 16 * (e >> 2) + (e & 3) >= vis.nv) p[e] = -INFINITY;
+        }
+        if constexpr (LOG) {
+            if (h0 + c < a.G) {
+                float* to = a.logits + ((int64_t)b * a.Hq + h) * a.ld + i0;   // ld holds whole tiles
+                *reinterpret_cast<float4*>(to) = make_float4(p[0], p[1], p[2], p[3]);
+                *reinterpret_cast<float4*>(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
+            }
+        }
+        float mx = p[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, p[e]);
+        const float m_new = fmaxf(m, max_x16_x32(mx));
+        if (__any(m_new > m)) {
+            const float al = exp2_ftz(m - m_new);
+            l *= al;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o[d] *= al;
+        }
+        m = m_new;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            p[e] = exp2_ftz(p[e] - m + kWeightShift<DT>);
+            l += p[e];
+        }
+        uint4 pt[kTerms];
+        split_weights<DT>(p, pt);
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+            const u32x2_v lo = read_transposed(vr + 16 * d), hi = read_transposed(vr + 16 * kVRow + 16 * d);
+            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+#pragma unroll
+            for (int u = 0; u < kTerms; ++u) o[d] = mfma16<DT>(vf, pt[u], o[d]);
+        }
+    }
+
+    // the four waves' outputs: (m, l) first, then the weighted sums
+    l = sum_x16_x32(l);
+    if (qd == 0) ml[w][c] = make_float2(m, l);
+    __syncthreads();
+    float M = -INFINITY, L = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) M = fmaxf(M, ml[u][c].x);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) L += ml[u][c].y > 0.0f ? ml[u][c].y * exp2_ftz(ml[u][c].x - M) : 0.0f;
+    const float mine = l > 0.0f ? exp2_ftz(m - M) : 0.0f;
+    float* ol = reinterpret_cast<float*>(vlds);        // [4][kHeads][kHeadDim]
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+        *reinterpret_cast<f32x4_v*>(ol + (w * kHeads + c) * kHeadDim + 16 * d + 4 * qd) = o[d] * mine;
+    if (tid < kHeads) {                                // lane c of wave 0 holds head c
+        inv_l[tid] = L > 0.0f ? 1.0f / L : 0.0f;       // nothing visible: 0
+        if (a.part_ml && h0 + tid < a.G)
+            a.part_ml[((int64_t)b * a.Hq + g * a.G + h0 + tid) * a.nsplit + split] = make_float2(M, L);
+    }
+    __syncthreads();
+    const int heads = min(kHeads, a.G - h0);
+    for (int e = tid; e < heads * (kHeadDim / 4); e += 256) {
+        const int hh = e / (kHeadDim / 4), d = e % (kHeadDim / 4) * 4;
+        f32x4_v s = *reinterpret_cast<const f32x4_v*>(ol + hh * kHeadDim + d);
+#pragma unroll
+        for (int u = 1; u < 4; ++u) s += *reinterpret_cast<const f32x4_v*>(ol + (u * kHeads + hh) * kHeadDim + d);
+        const int64_t bh = (int64_t)b * a.Hq + g * a.G + h0 + hh;
+        if (a.nsplit > 1) *reinterpret_cast<f32x4_v*>(a.part_o + (bh * a.nsplit + split) * kHeadDim + d) = s;
+        else *reinterpret_cast<f32x4_v*>(a.out + bh * kHeadDim + d) = s * inv_l[hh];
+    }
+}
+
+// One share per thread of a head at most (kMaxCacheSplits); empty shares have
+// l = 0, and a head without any l gives 0.
+__device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t bh, float* red, float* wgt, float* osum)
+{
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    float2 v = make_float2(-INFINITY, 0.0f);
+    if (tid < a.nsplit) v = a.part_ml[bh * a.nsplit + tid];
+    const float mx = wave_max(v.y > 0.0f ? v.x : -INFINITY);
+    if (lane == 0) red[w] = mx;
+    __syncthreads();
+    const float M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float x = v.y > 0.0f ? exp2_ftz(v.x - M) : 0.0f;
+    wgt[tid] = x;
+    const float ls = wave_sum(x * v.y);
+    if (lane == 0) red[4 + w] = ls;
+    __syncthreads();
+    const float L = (red[4] + red[5]) + (red[6] + red[7]);
+    const int d = tid & (kHeadDim - 1), half = tid / kHeadDim;
+    const float* po = a.part_o + bh * a.nsplit * kHeadDim + d;
+    float o = 0.0f;
+#pragma unroll 8
+    for (int s = half; s < a.nsplit; s += 2) o += wgt[s] * po[(int64_t)s * kHeadDim];
+    osum[tid] = o;
+    __syncthreads();
+    if (half == 0) a.out[bh * kHeadDim + d] = L > 0.0f ? (o + osum[tid + kHeadDim]) / L : 0.0f;
+}
+
+// S[b, r, j(i)] += the weights of the row's heads, 1024 positions per workgroup:
+// the heads' (m, l) from the shares first, then each thread four positions of
+// every head, in head order.
+__device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t block, float2* red, float2* stat)
+{
+    const int tid = threadIdx.x;
+    const int chunk = (int)(block % a.s_chunks);
+    const int64_t row = block / a.s_chunks;
+    const int b = (int)(row / a.R), r = (int)(row % a.R);
+    const int heads = a.R > 1 ? a.G : a.Hq;
+    const int64_t bh0 = (int64_t)b * a.Hq + (int64_t)r * a.G;
+    const Visible vis = visible(seq_len(a.lens, b, a.n), a.sink, a.window);
+    const int i = chunk * kScoreChunk + 4 * tid;
+    if (chunk * kScoreChunk >= vis.nv) return;           // the same for the whole workgroup
+    const int tph = 256 / heads;                         // threads per head (heads <= 256)
+    {
+        const int hh = tid / tph, sub = tid % tph;
+        float m = -INFINITY, l = 0.0f;
+        if (hh < heads) {
+            const float2* ml = a.part_ml + (bh0 + hh) * a.nsplit;
+#pragma unroll 8
+            for (int s = sub; s < a.nsplit; s += tph) {
+                const float2 v = ml[s];
+                if (v.y > 0.0f) {
+                    const float M = fmaxf(m, v.x);
+                    l = l * exp2_ftz(m - M) + v.y * exp2_ftz(v.x - M);
+                    m = M;
+                }
+            }
+        }
+        red[tid] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (tid < heads) {
+        float M = -INFINITY, L = 0.0f;
+        for (int u = 0; u < tph; ++u) M = fmaxf(M, red[tid * tph + u].x);
+        for (int u = 0; u < tph; ++u) {
+            const float2 v = red[tid * tph + u];
+            L += v.y > 0.0f ? v.y * exp2_ftz(v.x - M) : 0.0f;
+        }
+        // the shares' l carry the weights' factor
+        stat[tid] = make_float2(M - kWeightShift<0>, 1.0f / L);
+    }
+    __syncthreads();
+    if (i >= vis.nv) return;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float* x = a.logits + bh0 * a.ld + i;
+#pragma unroll 8
+    for (int hh = 0; hh < heads; ++hh) {
+        const float4 v = *reinterpret_cast<const float4*>(x + (int64_t)hh * a.ld);
+        const float2 st = stat[hh];
+        acc.x += exp2_ftz(v.x - st.x) * st.y;
+        acc.y += exp2_ftz(v.y - st.x) * st.y;
+        acc.z += exp2_ftz(v.z - st.x) * st.y;
+        acc.w += exp2_ftz(v.w - st.x) * st.y;
+    }
+    float* s = a.s + (int64_t)b * a.s_sb + (int64_t)r * a.s_sr;
+    const float e[4] = {acc.x, acc.y, acc.z, acc.w};
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (i + u < vis.nv) s[vis.token(i + u)] += e[u];
+}
+
+// The first merge_blocks workgroups join one head's shares each, the others add weights.
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a, int64_t merge_blocks)
+{
+    __shared__ float2 red[256];
+    __shared__ float2 stat[256];
+    if ((int64_t)blockIdx.x < merge_blocks)
+        merge_shares(a, blockIdx.x, reinterpret_cast<float*>(stat), reinterpret_cast<float*>(red),
+                     reinterpret_cast<float*>(red) + 256);
+    else
+        add_weights(a, (int64_t)blockIdx.x - merge_blocks, red, stat);
+}
+
+template <int KT>
+void launch_rows(const CacheAttnArgs& a, hipStream_t st)
+{
+    const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.head_tiles * a.nsplit));
+    if constexpr (KT == kRowsPacked) {
+        if (a.idx) hipLaunchKernelGGL((cache_attn_kernel<KT, true, false>), grid, dim3(256), 0, st, a);
+        else if (a.s) hipLaunchKernelGGL((cache_attn_kernel<KT, false, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((cache_attn_kernel<KT, false, false>), grid, dim3(256), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((cache_attn_kernel<KT, false, false>), grid, dim3(256), 0, st, a);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st)
+{
+    if (a.kc) launch_rows<kRowsPacked>(a, st);
+    else if (dtype == 1) launch_rows<kRowsBf16>(a, st);
+    else launch_rows<kRowsF16>(a, st);
+    if (hipError_t e = hipGetLastError()) return e;
+    const int64_t merge = a.nsplit > 1 ? (int64_t)a.B * a.Hq : 0, add = a.s ? (int64_t)a.B * a.R * a.s_chunks : 0;
+    if (merge + add == 0) return hipSuccess;
+    hipLaunchKernelGGL(cache_merge_kernel, dim3((unsigned)(merge + add)), dim3(256), 0, st, a, merge);
+    return hipGetLastError();
+}
+
+}  // namespace hill

@@ -613,6 +613,133 @@ hill_status run_step(const hill_desc* d, const void* q, const void* k, const voi
     return HILL_OK;
 }
 
+hill_status check_lens(const int32_t* lens)
+{
+    if ((uintptr_t)lens & 3u) return fail(HILL_ERR_INVALID_ARG, "lens is not 4-byte aligned");
+    return HILL_OK;
+}
+
+hill_status check_packed(const hill_packed* p, int64_t rows)
+{
+    if (!p) return fail(HILL_ERR_INVALID_ARG, "packed cache is NULL");
+    if (p->struct_size != sizeof(hill_packed))
+        return fail(HILL_ERR_INVALID_ARG, "struct_size %u != sizeof(hill_packed) %zu", p->struct_size, sizeof(hill_packed));
+    if (p->cap < 1 || p->cap < rows)
+        return fail(HILL_ERR_INVALID_ARG, "packed cache capacity %d must be >= 1 and >= %lld", p->cap, (long long)rows);
+    HILL_TRY(check_ptr(p->k_codes, "k_codes"));
+    HILL_TRY(check_ptr(p->k_params, "k_params"));
+    HILL_TRY(check_ptr(p->v_codes, "v_codes"));
+    HILL_TRY(check_ptr(p->v_params, "v_params"));
+    return HILL_OK;
+}
+
+// Launch grids hold 2^31 - 1 workgroups.
+hill_status check_grid(int64_t wgs)
+{
+    if (wgs > INT32_MAX) return fail(HILL_ERR_UNSUPPORTED, "batch and heads need %lld workgroups", (long long)wgs);
+    return HILL_OK;
+}
+
+// Shares and workspace of one token's dense attention: partial outputs
+// [B,Hq,nsplit,D], (max, sum) [B,Hq,nsplit], logits [B,Hq,ld], each 256-byte
+// aligned, as far as they are needed.
+struct CacheLayout {
+    int head_tiles, nsplit;
+    int64_t ld, wgs;
+    size_t part_o, part_ml, logits, end;
+};
+
+CacheLayout cache_layout(const hill_desc* d, const Shape& s, int ksel, bool with_s)
+{
+    CacheLayout L{};
+    int64_t seen = (int64_t)d->n_sink + d->n_recent;
+    if (ksel > 0) seen = ksel;
+    else if (seen > s.n) seen = s.n;
+    L.head_tiles = (s.G + 15) / 16;
+    L.nsplit = cache_splits((int64_t)s.B * s.Hkv * L.head_tiles, seen);
+    L.wgs = (int64_t)s.B * s.Hkv * L.head_tiles * L.nsplit;
+    L.ld = (seen + 31) / 32 * 32;
+    const size_t bh = (size_t)s.B * s.Hq;
+    size_t off = 0;
+    L.part_o = off;
+    if (L.nsplit > 1) off += align256(bh * L.nsplit * kHeadDim * sizeof(float));
+    L.part_ml = off;
+    if (L.nsplit > 1 || with_s) off += align256(bh * L.nsplit * sizeof(float2));
+    L.logits = off;
+    if (with_s) off += align256(bh * L.ld * sizeof(float));
+    L.end = off;
+    return L;
+}
+
+CacheAttnArgs cache_args(const hill_desc* d, const Shape& s, const CacheLayout& L, const void* q, const int32_t* lens,
+                         float* out, void* ws)
+{
+    CacheAttnArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_sb = d->q_stride_b;
+    a.q_sh = d->q_stride_h;
+    a.lens = lens;
+    a.B = s.B;
+    a.Hq = s.Hq;
+    a.Hkv = s.Hkv;
+    a.G = s.G;
+    a.R = s.R;
+    a.n = s.n;
+    a.sink = d->n_sink < s.n ? d->n_sink : s.n;           // more than the cache holds is all of it (no overflow
+    a.window = d->n_recent < s.n ? d->n_recent : s.n;     // on the device)
+    a.head_tiles = L.head_tiles;
+    a.nsplit = L.nsplit;
+    a.s2 = s.scale * 1.4426950408889634f;
+    if (L.nsplit > 1) {
+        a.part_o = at<float>(ws, L.part_o);
+        a.part_ml = at<float2>(ws, L.part_ml);
+    }
+    a.out = out;
+    return a;
+}
+
+void set_packed(const hill_packed* p, uint8_t** kc, uint8_t** vc, uint32_t** kp, uint32_t** vp)
+{
+    *kc = static_cast<uint8_t*>(p->k_codes);
+    *vc = static_cast<uint8_t*>(p->v_codes);
+    *kp = static_cast<uint32_t*>(p->k_params);
+    *vp = static_cast<uint32_t*>(p->v_params);
+}
+
+PackArgs pack_args(const hill_desc* d, const Shape& s, const hill_packed* p, void* k, void* v)
+{
+    PackArgs a{};
+    a.k = static_cast<uint16_t*>(k);
+    a.v = static_cast<uint16_t*>(v);
+    a.k_sb = d->k_stride_b;
+    a.k_sh = d->k_stride_h;
+    a.k_sn = d->k_stride_n;
+    a.v_sb = d->v_stride_b;
+    a.v_sh = d->v_stride_h;
+    a.v_sn = d->v_stride_n;
+    set_packed(p, &a.kc, &a.vc, &a.kp, &a.vp);
+    a.cap = p->cap;
+    a.B = s.B;
+    a.Hkv = s.Hkv;
+    return a;
+}
+
+// The selection's regions without those of the scores, then the eviction's flags.
+Shape evict_shape(Shape s)
+{
+    s.mode = HILL_SCORE_RAW;
+    s.gran = HILL_SEL_KVHEAD;
+    return s;
+}
+
+int64_t evict_chunks(int k_keep) { return (k_keep + kEvictChunk - 1) / kEvictChunk; }
+
+size_t evict_bytes(const Shape& s, int k_keep, size_t* flags)
+{
+    *flags = layout_for(evict_shape(s), k_keep).end_topk;
+    return *flags + align256((1 + (size_t)s.B * s.Hkv * evict_chunks(k_keep)) * sizeof(uint32_t));
+}
+
 }  // namespace
 
 extern "C" {
@@ -738,6 +865,266 @@ hill_status check_bkp(const hill_bkp_desc* d)
     if (d->stride_r < d->n_tokens) return fail(HILL_ERR_INVALID_ARG, "stride_r must be >= n_tokens");
     if (d->batch > 1 && d->stride_b < (int64_t)d->rows * d->stride_r)
         return fail(HILL_ERR_INVALID_ARG, "stride_b must be >= rows * stride_r");
+    return HILL_OK;
+}
+
+hill_status hill_window_workspace_bytes(const hill_desc* d, int32_t n_new, size_t* bytes)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    if (n_new < 0 || n_new > s.n) return fail(HILL_ERR_INVALID_ARG, "n_new %d not in [0, n_tokens=%d]", n_new, s.n);
+    if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = n_new == 0 ? cache_layout(d, s, 0, false).end : 0;
+    return HILL_OK;
+}
+
+hill_status hill_window_attn(const hill_desc* d, const void* q, const void* k, const void* v, const int32_t* lens, float* out,
+                             void* ws, size_t ws_bytes, void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    HILL_TRY(check_ptr(q, "q"));
+    HILL_TRY(check_ptr(k, "k"));
+    HILL_TRY(check_ptr(v, "v"));
+    HILL_TRY(check_lens(lens));
+    HILL_TRY(check_ptr(out, "out"));
+    const CacheLayout L = cache_layout(d, s, 0, false);
+    HILL_TRY(check_grid(L.wgs));
+    HILL_TRY(check_ws(ws, ws_bytes, L.end));
+    CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.k_sb = d->k_stride_b;
+    a.k_sh = d->k_stride_h;
+    a.k_sn = d->k_stride_n;
+    a.v_sb = d->v_stride_b;
+    a.v_sh = d->v_stride_h;
+    a.v_sn = d->v_stride_n;
+    HIP_TRY(launch_cache_attn(a, s.dtype, static_cast<hipStream_t>(stream)));
+    return HILL_OK;
+}
+
+hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, const void* q, const void* k, const void* v,
+                                const int32_t* lens, void* out, void* ws, size_t ws_bytes, void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    if (!p) return fail(HILL_ERR_INVALID_ARG, "prefill descriptor is NULL");
+    if (p->struct_size != sizeof(hill_prefill_desc))
+        return fail(HILL_ERR_INVALID_ARG, "struct_size %u != sizeof(hill_prefill_desc) %zu", p->struct_size,
+                    sizeof(hill_prefill_desc));
+    if (p->n_new < 1 || p->n_new > s.n)
+        return fail(HILL_ERR_INVALID_ARG, "n_new %d not in [1, n_tokens=%d]", p->n_new, s.n);
+    const int64_t st[] = {p->q_stride_t, p->o_stride_b, p->o_stride_h, p->o_stride_t};
+    for (int64_t x : st)
+        if (x < 0 || x % 8) return fail(HILL_ERR_INVALID_ARG, "q_stride_t and out strides must be non-negative multiples of 8");
+    if ((p->n_new > 1 && (p->q_stride_t < s.D || p->o_stride_t < s.D)) || (s.Hq > 1 && p->o_stride_h < s.D) ||
+        (s.B > 1 && p->o_stride_b < s.D))
+        return fail(HILL_ERR_INVALID_ARG, "q_stride_t or an out stride < head_dim");
+    HILL_TRY(check_ptr(q, "q"));
+    HILL_TRY(check_ptr(k, "k"));
+    HILL_TRY(check_ptr(v, "v"));
+    HILL_TRY(check_lens(lens));
+    HILL_TRY(check_ptr(out, "out"));
+    HILL_TRY(check_ws(ws, ws_bytes, 0));
+    const int64_t blocks = ((int64_t)p->n_new * s.G + kPrefillRows - 1) / kPrefillRows;
+    HILL_TRY(check_grid((int64_t)s.B * s.Hkv * blocks));
+    PrefillArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.out = static_cast<uint16_t*>(out);
+    a.q_sb = d->q_stride_b;
+    a.q_sh = d->q_stride_h;
+    a.q_st = p->q_stride_t;
+    a.o_sb = p->o_stride_b;
+    a.o_sh = p->o_stride_h;
+    a.o_st = p->o_stride_t;
+    a.k_sb = d->k_stride_b;
+    a.k_sh = d->k_stride_h;
+    a.k_sn = d->k_stride_n;
+    a.v_sb = d->v_stride_b;
+    a.v_sh = d->v_stride_h;
+    a.v_sn = d->v_stride_n;
+    a.lens = lens;
+    a.B = s.B;
+    a.Hq = s.Hq;
+    a.Hkv = s.Hkv;
+    a.G = s.G;
+    a.n = s.n;
+    a.t = p->n_new;
+    a.sink = d->n_sink < s.n ? d->n_sink : s.n;           // more than the cache holds is all of it (no overflow
+    a.window = d->n_recent < s.n ? d->n_recent : s.n;     // on the device)
+    a.blocks = (int)blocks;
+    a.s2 = s.scale * 1.4426950408889634f;
+    HIP_TRY(launch_prefill(a, s.dtype, static_cast<hipStream_t>(stream)));
+    return HILL_OK;
+}
+
+hill_status hill_pack_kv(const hill_desc* d, const hill_packed* p, const void* k, const void* v, const int32_t* at,
+                         int32_t at0, void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    HILL_TRY(check_packed(p, 1));
+    HILL_TRY(check_ptr(k, "k"));
+    HILL_TRY(check_ptr(v, "v"));
+    if ((uintptr_t)at & 3u) return fail(HILL_ERR_INVALID_ARG, "at is not 4-byte aligned");
+    if (!at && (at0 < 0 || (int64_t)at0 + s.n > p->cap))
+        return fail(HILL_ERR_INVALID_ARG, "rows [%d, %lld) not inside [0, cap=%d)", at0, (long long)at0 + s.n, p->cap);
+    PackArgs a = pack_args(d, s, p, const_cast<void*>(k), const_cast<void*>(v));
+    a.at = at;
+    a.at0 = at0;
+    a.rows = s.n;
+    HIP_TRY(launch_pack(a, s.dtype, static_cast<hipStream_t>(stream)));
+    return HILL_OK;
+}
+
+hill_status hill_unpack_kv(const hill_desc* d, const hill_packed* p, int32_t token_begin, int32_t token_end, void* k, void* v,
+                           void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    HILL_TRY(check_packed(p, 1));
+    HILL_TRY(check_ptr(k, "k"));
+    HILL_TRY(check_ptr(v, "v"));
+    if (token_begin < 0 || token_begin > token_end || token_end > p->cap)
+        return fail(HILL_ERR_INVALID_ARG, "token range [%d, %d) not inside [0, cap=%d)", token_begin, token_end, p->cap);
+    if (token_end - token_begin > s.n)
+        return fail(HILL_ERR_INVALID_ARG, "%d rows do not fit n_tokens %d", token_end - token_begin, s.n);
+    if (token_begin == token_end) return HILL_OK;
+    PackArgs a = pack_args(d, s, p, k, v);
+    a.at0 = token_begin;
+    a.rows = token_end - token_begin;
+    HIP_TRY(launch_unpack(a, s.dtype, static_cast<hipStream_t>(stream)));
+    return HILL_OK;
+}
+
+hill_status hill_packed_workspace_bytes(const hill_desc* d, int32_t k_sel, int32_t with_s, size_t* bytes)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    if (k_sel != 0) HILL_TRY(check_ksel(s, k_sel));
+    if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = cache_layout(d, s, k_sel, with_s != 0).end;
+    return HILL_OK;
+}
+
+hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, const void* q, const int32_t* lens,
+                             const int32_t* idx, int32_t k_sel, float* s_acc, float* out, void* ws, size_t ws_bytes,
+                             void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, s_acc != nullptr));
+    HILL_TRY(check_packed(p, s.n));
+    HILL_TRY(check_ptr(q, "q"));
+    HILL_TRY(check_lens(lens));
+    if (idx) {
+        HILL_TRY(check_ksel(s, k_sel));
+        if ((uintptr_t)idx & 3u) return fail(HILL_ERR_INVALID_ARG, "idx is not 4-byte aligned");
+        if (lens || s_acc) return fail(HILL_ERR_INVALID_ARG, "lens and s do not go with idx");
+    } else if (k_sel != 0) {
+        return fail(HILL_ERR_INVALID_ARG, "k_sel %d without idx", k_sel);
+    }
+    if (s_acc) HILL_TRY(check_ptr(s_acc, "s"));
+    HILL_TRY(check_ptr(out, "out"));
+    const CacheLayout L = cache_layout(d, s, idx ? k_sel : 0, s_acc != nullptr);
+    const int s_chunks = (int)((L.ld + kScoreChunk - 1) / kScoreChunk);
+    HILL_TRY(check_grid(L.wgs + (int64_t)s.B * s.Hq + (int64_t)s.B * s.R * s_chunks));
+    HILL_TRY(check_ws(ws, ws_bytes, L.end));
+    CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
+    uint8_t *kc, *vc;
+    uint32_t *kp, *vp;
+    set_packed(p, &kc, &vc, &kp, &vp);
+    a.kc = kc;
+    a.vc = vc;
+    a.kp = kp;
+    a.vp = vp;
+    a.cap = p->cap;
+    a.q_bf16 = s.dtype == HILL_BF16;
+    a.idx = idx;
+    a.ksel = k_sel;
+    if (s_acc) {
+        a.part_ml = at<float2>(ws, L.part_ml);
+        a.s = s_acc;
+        a.s_sb = d->s_stride_b;
+        a.s_sr = d->s_stride_r;
+        a.logits = at<float>(ws, L.logits);
+        a.ld = L.ld;
+        a.s_chunks = s_chunks;
+    }
+    HIP_TRY(launch_cache_attn(a, s.dtype, static_cast<hipStream_t>(stream)));
+    return HILL_OK;
+}
+
+hill_status hill_evict_workspace_bytes(const hill_desc* d, int32_t k_keep, size_t* bytes)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s, false));
+    HILL_TRY(check_ksel(s, k_keep));
+    if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
+    size_t flags;
+    *bytes = evict_bytes(s, k_keep, &flags);
+    return HILL_OK;
+}
+
+hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t* idx_out, void* k, void* v,
+                       const hill_packed* p, int32_t* pos, void* ws, size_t ws_bytes, void* stream)
+{
+    Shape s;
+    HILL_TRY(check_desc(d, &s));
+    HILL_TRY(check_ksel(s, k_keep));
+    HILL_TRY(check_pins(s, k_keep));
+    HILL_TRY(check_ptr(s_acc, "s"));
+    if (!idx_out || ((uintptr_t)idx_out & 3u)) return fail(HILL_ERR_INVALID_ARG, "idx_out is NULL or not 4-byte aligned");
+    if ((uintptr_t)pos & 3u) return fail(HILL_ERR_INVALID_ARG, "pos is not 4-byte aligned");
+    if (!k != !v) return fail(HILL_ERR_INVALID_ARG, "k and v go together");
+    if (k && p) return fail(HILL_ERR_INVALID_ARG, "k and v, or a packed cache, not both");
+    if (k) {
+        HILL_TRY(check_ptr(k, "k"));
+        HILL_TRY(check_ptr(v, "v"));
+        if ((s.Hkv > 1 && (d->k_stride_h < s.D || d->v_stride_h < s.D)) ||
+            (s.B > 1 && (d->k_stride_b < s.D || d->v_stride_b < s.D)))
+            return fail(HILL_ERR_INVALID_ARG, "rows of k or v overlap");
+    }
+    if (p) HILL_TRY(check_packed(p, s.n));
+    size_t flags;
+    const size_t need = evict_bytes(s, k_keep, &flags);
+    const int64_t chunks = evict_chunks(k_keep);
+    const int heads = k || p ? s.Hkv : s.R;
+    HILL_TRY(check_grid(s.B * heads * chunks));
+    HILL_TRY(check_ws(ws, ws_bytes, need));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Layout L = layout_for(evict_shape(s), k_keep);
+    EvictArgs a{};
+    a.flags = at<uint32_t>(ws, flags);
+    HIP_TRY(launch_fill_zero(a.flags, 1 + s.B * heads * chunks, st));
+    HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st));
+    a.idx = idx_out;
+    a.B = s.B;
+    a.R = s.R;
+    a.Hkv = s.Hkv;
+    a.n = s.n;
+    a.keep = k_keep;
+    a.s = s_acc;
+    a.pos = pos;
+    a.s_sb = d->s_stride_b;
+    a.s_sr = d->s_stride_r;
+    a.k = static_cast<uint16_t*>(k);
+    a.v = static_cast<uint16_t*>(v);
+    a.k_sb = d->k_stride_b;
+    a.k_sh = d->k_stride_h;
+    a.k_sn = d->k_stride_n;
+    a.v_sb = d->v_stride_b;
+    a.v_sh = d->v_stride_h;
+    a.v_sn = d->v_stride_n;
+    if (p) {
+        set_packed(p, &a.kc, &a.vc, &a.kp, &a.vp);
+        a.cap = p->cap;
+    }
+    a.heads = heads;
+    a.chunks = (int)chunks;
+    HIP_TRY(launch_evict(a, st));
     return HILL_OK;
 }
 

@@ -392,6 +392,101 @@ constexpr int kRowTopkTokens = 32768;
 hipError_t launch_row_attend(const RefineArgs& r, const AttnArgs& at, int dtype, int32_t* idx, hipStream_t st,
                              Stamp ts = {});
 hipError_t launch_row_topk(const RefineArgs& r, int rows, int32_t* idx, float* val, hipStream_t st);
+// One token's dense attention over a 16-bit or a packed cache (cache_attn.hip).
+struct CacheAttnArgs {
+    const uint16_t* q;
+    int64_t q_sb, q_sh;
+    const uint16_t* k;        // 16-bit rows
+    const uint16_t* v;
+    int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+    const uint8_t* kc;        // nullable: packed rows instead, codes [B,Hkv,cap,64]
+    const uint8_t* vc;
+    const uint32_t* kp;       //   and (scale, zero) per group [B,Hkv,cap,4]
+    const uint32_t* vp;
+    int64_t cap;
+    int q_bf16;               //   q is bf16
+    const int32_t* lens;      // nullable: [B] tokens per sequence, instead of n
+    const int32_t* idx;       // nullable (packed): [B,R,ksel] tokens instead of the visible ones
+    int ksel;
+    int B, Hq, Hkv, G, R, n, sink, window;
+    int head_tiles, nsplit;   // 16-head tiles per KV head; shares of the visible positions
+    float s2;
+    float* part_o;            // [B,Hq,nsplit,D] (nsplit > 1)
+    float2* part_ml;          // [B,Hq,nsplit] (max, sum) in the exp2 domain (nsplit > 1 or s)
+    float* out;               // [B,Hq,D]
+    float* s;                 // nullable (packed, no idx): S += the weights
+    int64_t s_sb, s_sr;
+    float* logits;            //   [B,Hq,ld] by visible position, ld a multiple of 32
+    int64_t ld;
+    int s_chunks;             //   kScoreChunk-position chunks per row
+};
+constexpr int kMaxCacheSplits = 256;   // one per thread of the merge
+constexpr int kScoreChunk = 1024;
+// Shares of `seen` visible positions: until about three workgroups per CU run
+// (of 256), each of at least four 32-token tiles, one per wave.
+inline int cache_splits(int64_t wgs, int64_t seen)
+{
+    const int64_t want = (768 + wgs - 1) / wgs, most = (seen + 127) / 128;
+    const int64_t s = want < most ? want : most;
+    return s < 1 ? 1 : s > kMaxCacheSplits ? kMaxCacheSplits : (int)s;
+}
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
+
+// Rows of T tokens into, and out of, the 4-bit cache (packed.hip).
+struct PackArgs {
+    uint16_t* k;              // source (pack) or destination (unpack) rows
+    uint16_t* v;
+    int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+    uint8_t* kc;
+    uint8_t* vc;
+    uint32_t* kp;
+    uint32_t* vp;
+    int64_t cap;
+    const int32_t* at;        // nullable: [B] cache position of each sequence's first row, instead of at0
+    int at0;
+    int B, Hkv, rows;
+};
+hipError_t launch_pack(const PackArgs& a, int dtype, hipStream_t st);
+hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t st);
+
+// Attention of a chunk's T tokens over the first tokens and a sliding window (prefill.hip).
+struct PrefillArgs {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    uint16_t* out;
+    int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st;
+    int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+    const int32_t* lens;
+    int B, Hq, Hkv, G, n, t, sink, window;
+    int blocks;               // row blocks per (b, KV head)
+    float s2;
+};
+constexpr int kPrefillRows = 128;   // (token, head) rows per workgroup
+hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st);
+
+// Kept rows moved to the front (evict.hip).
+struct EvictArgs {
+    const int32_t* idx;       // [B,R,keep] ascending
+    int B, R, Hkv, n, keep;
+    float* s;
+    int32_t* pos;             // nullable, strides of s
+    int64_t s_sb, s_sr;
+    uint16_t* k;              // nullable, with v
+    uint16_t* v;
+    int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+    uint8_t* kc;              // nullable, with the other three
+    uint8_t* vc;
+    uint32_t* kp;
+    uint32_t* vp;
+    int64_t cap;
+    uint32_t* flags;          // [1 + B * heads * chunks]: a ticket counter, then chunks whose sources have been read; zeroed
+    int heads;                // row groups per sequence that move: Hkv, or R without K and V
+    int chunks;
+};
+constexpr int kEvictChunk = 64;   // kept rows per workgroup
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
+
 hipError_t launch_attn_split(const AttnArgs& a, int dtype, hipStream_t st);
 hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t st, Stamp ts = {});
 

@@ -1,0 +1,221 @@
+// Attention of a chunk's tokens over the first tokens and a sliding window.
+//
+// The rows of a (sequence, KV head) are its T tokens times its G query heads,
+// token by token: a workgroup takes 128 of them (four waves of 32), so that a
+// group's heads share the keys and values they read and the rows of a workgroup lie
+// at few positions, whatever G.  It walks the first tokens and then the window
+// [first position - window + 1, last position] in tiles of 64, double-buffered in LDS by
+// direct loads, with running maxima and sums:
+//
+//   x^T = K Q^T on the matrix cores (tokens x rows): a lane holds one row's
+//   logits, the maximum needs one exchange between lane halves, and the weights
+//   are, rounded to 16 bits, the second product's operand as they lie;
+//   O^T += V^T w^T with V read from LDS transposed.
+//
+// The bound is the matrix cores, with the exponentials close behind.  Weights
+// are rounded to the cache's type (the output is rounded to it anyway); maxima,
+// sums and O are fp32.  The reference of the exponentials follows the running
+// maximum only when that has grown by more than 2^8: weights stay below 2^8 and
+// O is rescaled rarely.
+#include "mfma_device.h"
+
+namespace hill {
+
+namespace {
+
+constexpr int kKeys = 64;                       // tokens per tile
+constexpr int kTileHalfs = kKeys * kHeadDim;    // 16-bit elements of a K or V tile
+constexpr float kSlack = 8.0f;
+
+// Rows of a tile are 16 pieces of 16 bytes; row j keeps piece c at c ^ swizzle(j), so that the rows that one LDS
+// access touches (16 in a column of K, four by four of V) lie in different banks.
+__device__ __forceinline__ int swizzle(int j) { return ((j & 3) << 2) | ((j >> 2) & 3); }
+
+__device__ __forceinline__ float max_x32(float v)
+{
+    auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+template <int DT>
+__device__ __forceinline__ uint32_t round_pair(float x, float y)
+{
+    if constexpr (DT == 1) return __builtin_bit_cast(uint32_t, bf162_t{(__bf16)x, (__bf16)y});
+    else return __builtin_bit_cast(uint32_t, half2_t{(_Float16)x, (_Float16)y});
+}
+
+// 16 bytes per lane from global memory into LDS, lane after lane from `to` on.
+__device__ __forceinline__ void load_lds16(const uint16_t* from, uint16_t* to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+template <int DT>
+__global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][kTileHalfs];   // [buffer][K, V]
+    const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hf = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (sequence, KV head) fastest, so that its blocks meet its K and V in one L2; the last tokens, whose windows
+    // are full, first
+    const int bh = blockIdx.x % (a.B * a.Hkv), blk = a.blocks - 1 - (int)(blockIdx.x / (a.B * a.Hkv));
+    const int b = bh / a.Hkv, g = bh % a.Hkv;
+    const int len = seq_len(a.lens, b, a.n);
+    const int first = len - a.t;                            // position of the chunk's first token (may be < 0)
+    const int rows = a.t * a.G;
+    const int r0 = blk * kPrefillRows;
+    const int row = min(r0 + 32 * w + c32, rows - 1);       // this lane's row
+    const int tq = row / a.G, hq = g * a.G + row % a.G;
+    const int p = first + tq;
+    const int pa = max(first + r0 / a.G, 0), pb = first + min(r0 + kPrefillRows - 1, rows - 1) / a.G;
+
+    uint16_t* out = a.out + (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)tq * a.o_st;
+    const bool live = r0 + 32 * w + c32 < rows;
+
+    f32x16_v o[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    if (pb >= 0) {
+        // tokens [0, ns) and [ws, pb]
+        const int ws = max(pa - a.window + 1, 0);
+        const int ns = min(a.sink, ws);
+        const int st = (ns + kKeys - 1) / kKeys, nt = st + (pb + 1 - ws + kKeys - 1) / kKeys;
+        const int pw0 = __builtin_amdgcn_readfirstlane(p), pw1 = __builtin_amdgcn_readlane(p, 31);   // this wave's positions
+        const uint16_t* kb = a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh;
+        const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh;
+        auto tile_begin = [&](int t) { return t < st ? t * kKeys : ws + (t - st) * kKeys; };
+        auto tile_end = [&](int t) { return t < st ? min(ns, (t + 1) * kKeys) : min(pb + 1, ws + (t - st + 1) * kKeys); };
+        auto load = [&](int t) {   // rows past the tile's end repeat its last one (they weigh 0)
+            const int j0 = tile_begin(t), jl = tile_end(t) - 1;
+            uint16_t* kl = lds[t & 1][0];
+            uint16_t* vl = lds[t & 1][1];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int jr = 16 * u + 4 * w + (lane >> 4);
+                const int piece = (lane & 15) ^ swizzle(jr);
+                const uint32_t j = (uint32_t)min(j0 + jr, jl);
+                load_lds16(kb + (uint64_t)j * (uint32_t)a.k_sn + piece * 8, kl + (16 * u + 4 * w) * kHeadDim);
+                load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + (16 * u + 4 * w) * kHeadDim);
+            }
+        };
+        load(0);
+        uint4 qf[8];
+        const float s2 = fabsf(a.s2);                   // a negative scale goes into the query's signs
+        const uint32_t flip = a.s2 < 0.0f ? 0x80008000u : 0u;
+        const uint16_t* qr = a.q + (int64_t)b * a.q_sb + (int64_t)hq * a.q_sh + (int64_t)tq * a.q_st + 8 * hf;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            qf[i] = *reinterpret_cast<const uint4*>(qr + 16 * i);
+            qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
+        }
+
+        // this lane's LDS offsets (elements): K piece (2i + hf) of row c32 (+ 32), V rows 4 hf + (c16 / 4) on
+        const int c16 = lane & 15, vrow = 4 * hf + (c16 >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((c16 & 3) >> 1);
+        for (int t = 0; t < nt; ++t) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();       // tile t is there, and every wave has left tile t - 1
+            if (t + 1 < nt) load(t + 1);
+            const int j0 = tile_begin(t), j1 = tile_end(t);
+            // nothing of the tile visible to this wave's rows
+            if (j0 > pw1 || (j0 >= a.sink && j1 - 1 <= pw0 - a.window)) continue;
+            const uint16_t* kl = lds[t & 1][0];
+            const uint16_t* vl = lds[t & 1][1];
+            f32x16_v x[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[s][e] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int jr = 32 * s + c32;
+                    const uint4 kf = *reinterpret_cast<const uint4*>(kl + jr * kHeadDim + (((2 * i + hf) ^ swizzle(jr)) * 8));
+                    x[s] = mfma32<DT>(kf, qf[i], x[s]);
+                }
+            }
+            // every row of the wave sees the whole tile, or masks
+            const bool whole = j1 - j0 == kKeys && j1 - 1 <= pw0 && (j1 <= a.sink || j0 > pw1 - a.window);
+            float mx = -INFINITY;
+            if (whole) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[s][e]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = j0 + 32 * s + 4 * hf + (e & 3) + 8 * (e >> 2);
+                        const bool seen = j < j1 && j <= p && (j < a.sink || j > p - a.window);
+                        x[s][e] = seen ? x[s][e] : -INFINITY;
+                        mx = fmaxf(mx, x[s][e]);
+                    }
+            }
+            mx = max_x32(mx) * s2;
+            const bool grown = mx > m + kSlack;                 // m = -inf: the first visible tile
+            if (__any(grown)) {
+                const float m_new = grown ? mx : m;
+                const float al = grown ? exp2_ftz(m - m_new) : 1.0f;
+                m = m_new;
+                l *= al;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) o[d] *= al;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;        // a row that has seen nothing yet: weights 0
+            uint4 pf[4];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int h8 = 0; h8 < 2; ++h8) {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y0 = exp2_ftz(__builtin_fmaf(x[s][8 * h8 + 2 * e], s2, -ref));
+                        const float y1 = exp2_ftz(__builtin_fmaf(x[s][8 * h8 + 2 * e + 1], s2, -ref));
+                        l += y0 + y1;
+                        u[e] = round_pair<DT>(y0, y1);
+                    }
+                    pf[2 * s + h8] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {                       // 16 tokens each
+                const int ja = 16 * q + vrow, jb = ja + 8;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int piece = 4 * d + vpiece;
+                    const u32x2_v lo = read_transposed(vl + ja * kHeadDim + ((piece ^ swizzle(ja)) * 8) + 4 * (c16 & 1));
+                    const u32x2_v hi = read_transposed(vl + jb * kHeadDim + ((piece ^ swizzle(jb)) * 8) + 4 * (c16 & 1));
+                    o[d] = mfma32<DT>(make_uint4(lo.x, lo.y, hi.x, hi.y), pf[q], o[d]);
+                }
+            }
+        }
+    }
+    l += __shfl_xor(l, 32, 64);
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;               // nothing visible: 0
+    if (!live) return;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x0 = round_pair<DT>(o[d][4 * e] * inv, o[d][4 * e + 1] * inv);
+            const uint32_t x1 = round_pair<DT>(o[d][4 * e + 2] * inv, o[d][4 * e + 3] * inv);
+            *reinterpret_cast<uint2*>(out + 32 * d + 8 * e + 4 * hf) = make_uint2(x0, x1);
+        }
+}
+
+}  // namespace
+
+hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st)
+{
+    const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.blocks));
+    if (dtype == 1) hipLaunchKernelGGL(prefill_kernel<1>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(prefill_kernel<0>, grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace hill

@@ -35,12 +35,13 @@ DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 MODES = {"attn": 0, "raw": 1}
 GRANS = {"token": 0, "kvhead": 1}
 
-ABI_VERSION = 6   # HILL_ABI_VERSION of include/hill.h that this binding's structures follow
+ABI_VERSION = 7   # HILL_ABI_VERSION of include/hill.h that this binding's structures follow
 EXPORTS = ("hill_abi_version", "hill_status_str", "hill_last_error", "hill_workspace_bytes", "hill_score",
            "hill_topk", "hill_gather_attn", "hill_step", "hill_step_profiled", "hill_sketch_keys",
            "hill_score_sketch", "hill_step_sketch", "hill_bkp_workspace_bytes",
            "hill_bkp_update", "hill_app_balance", "hill_step_streamed", "hill_step_noalloc", "hill_tier_apply",
-           "hill_step_tiered")
+           "hill_step_tiered", "hill_window_workspace_bytes", "hill_window_attn", "hill_window_prefill", "hill_pack_kv",
+           "hill_unpack_kv", "hill_packed_workspace_bytes", "hill_packed_attn", "hill_evict_workspace_bytes", "hill_evict")
 
 
 class HillError(RuntimeError):
@@ -108,6 +109,18 @@ class TierDesc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("capacity", ctypes.c_int32), ("n_cap", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("hot_stride_b", ctypes.c_int64), ("hot_stride_h", ctypes.c_int64),
                 ("hot_stride_n", ctypes.c_int64)]
+
+
+class PrefillDesc(ctypes.Structure):
+    """hill_prefill_desc (include/hill.h)."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n_new", ctypes.c_int32), ("q_stride_t", ctypes.c_int64),
+                ("o_stride_b", ctypes.c_int64), ("o_stride_h", ctypes.c_int64), ("o_stride_t", ctypes.c_int64)]
+
+
+class PackedDesc(ctypes.Structure):
+    """hill_packed (include/hill.h)."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("cap", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("k_codes", "k_params", "v_codes", "v_params")]
 
 
 class AppParams(ctypes.Structure):
@@ -180,6 +193,18 @@ def load_library(path: str = LIB_PATH):
         lib.hill_step_tiered.restype = ctypes.c_int
         lib.hill_app_balance.argtypes = [ctypes.POINTER(AppParams), ctypes.POINTER(AppPlan)]
         lib.hill_app_balance.restype = ctypes.c_int
+        K, SZP = ctypes.POINTER(PackedDesc), ctypes.POINTER(SZ)
+        for name, args in (("hill_window_workspace_bytes", [D, I32, SZP]),
+                           ("hill_window_attn", [D, P, P, P, P, P, P, SZ, P]),
+                           ("hill_window_prefill", [D, ctypes.POINTER(PrefillDesc), P, P, P, P, P, P, SZ, P]),
+                           ("hill_pack_kv", [D, K, P, P, P, I32, P]),
+                           ("hill_unpack_kv", [D, K, I32, I32, P, P, P]),
+                           ("hill_packed_workspace_bytes", [D, I32, I32, SZP]),
+                           ("hill_packed_attn", [D, K, P, P, P, I32, P, P, P, SZ, P]),
+                           ("hill_evict_workspace_bytes", [D, I32, SZP]),
+                           ("hill_evict", [D, P, I32, P, P, P, K, P, P, SZ, P])):
+            getattr(lib, name).argtypes = args
+            getattr(lib, name).restype = ctypes.c_int
         if lib.hill_abi_version() != ABI_VERSION:
             raise RuntimeError("libhill.so has ABI version %d, this binding needs %d; rebuild it"
                                % (lib.hill_abi_version(), ABI_VERSION))
