@@ -408,7 +408,8 @@ HILL_API hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, 
  *   p        a packed cache (n_tokens <= cap), or neither;
  *   s        the importance, whose entries [k_keep, n_tokens) become 0, as hill_score
  *            wants them for tokens to come;
- *   pos      NULL, or int32 with S's strides, such as the tokens' positions.
+ *   pos      NULL, or int32 [B, R, >= n_tokens] with strides (pos_stride_b,
+ *            pos_stride_r) and contiguous tokens, such as the tokens' positions.
  * All KV heads of a sequence keep the same tokens (HILL_SEL_TOKEN) or each its own
  * (HILL_SEL_KVHEAD).  Other rows of k, v, p and pos from k_keep on are left as they
  * were.  The order of tokens stays, so the first n_sink and the last tokens are
@@ -417,7 +418,8 @@ HILL_API hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, 
  * a streamed selection goes on with a zeroed state. */
 HILL_API hill_status hill_evict_workspace_bytes(const hill_desc* d, int32_t k_keep, size_t* bytes);
 HILL_API hill_status hill_evict(const hill_desc* d, float* s, int32_t k_keep, int32_t* idx_out, void* k, void* v,
-                       const hill_packed* p, int32_t* pos, void* ws, size_t ws_bytes, void* stream);
+                       const hill_packed* p, int32_t* pos, int64_t pos_stride_b, int64_t pos_stride_r, void* ws,
+                       size_t ws_bytes, void* stream);
 
 /* Bidirectional KV Cache Pools (Sec. 4.2, HKM / BKP): the per-token hit-rate
  * table and the hot/cold pool policy, run once after each decoding step (the

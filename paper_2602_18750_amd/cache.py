@@ -320,9 +320,11 @@ def hill_evict(s, k_keep, *, k=None, v=None, cache: Optional[PackedCache] = None
     if R != (1 if granularity == "token" else Hkv):
         raise ValueError("s has %d rows per sequence, granularity %s needs %d" % (R, granularity, 1 if granularity == "token"
                                                                                   else Hkv))
-    if pos is not None and (pos.dtype != torch.int32 or pos.dim() != 3 or pos.shape[:2] != s.shape[:2] or
-                            pos.shape[2] < n or pos.stride() != s.stride()):
-        raise ValueError("pos must be int32 with the shape and strides of s")
+    p_st = (0, 0)
+    if pos is not None:
+        p_st = _rows("pos", pos, 3, torch.int32)
+        if pos.shape[:2] != s.shape[:2] or pos.shape[2] < n:
+            raise ValueError("pos must be [%d, %d, >= %d], not %s" % (B, R, n, tuple(pos.shape)))
     d = _desc(B, Hkv, Hkv, 128, n, dtype, k_st=k_st, v_st=v_st, s_st=s_st, granularity=granularity,
               n_sink=_count("n_sink", n_sink), n_recent=_count("n_recent", n_recent))
     with _on(dev, stream):
@@ -333,7 +335,7 @@ def hill_evict(s, k_keep, *, k=None, v=None, cache: Optional[PackedCache] = None
         ref = ctypes.byref(d)
         ws, ws_bytes = _workspace(lib.hill_evict_workspace_bytes, (ref, k_keep), dev, ws)
         _check(lib.hill_evict(ref, s.data_ptr(), k_keep, idx_out.data_ptr(), _ptr(k), _ptr(v),
-                              None if cache is None else ctypes.byref(cache.desc), _ptr(pos), _ptr(ws), ws_bytes,
+                              None if cache is None else ctypes.byref(cache.desc), _ptr(pos), *p_st, _ptr(ws), ws_bytes,
                               _stream_ptr(None)))
     return idx_out
 

@@ -41,6 +41,10 @@ struct TileRegs {
     uint32_t kp[2], vp[2];       // packed: (scale, zero) of the codes above
 };
 
+// Tiles that a wave requests ahead of the one it works on.
+template <int KT>
+constexpr int kTilesAhead = KT == kRowsPacked ? 2 : 1;
+
 // Tokens are taken into [0, n), so that a bad list entry reads a valid row.
 template <int KT, bool IDX>
 __device__ __forceinline__ void load_tile(const CacheAttnArgs& a, int b, int g, const Visible& vis, int i0, int tok,
@@ -157,7 +161,7 @@ __device__ __forceinline__ float bf16_query_to_half(uint4 (&qf)[4])
 }
 
 template <int KT, bool IDX, bool LOG>
-__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int DT = KT == kRowsBf16 ? 1 : 0;
     constexpr int kTerms = kWeightTerms<DT>;
@@ -210,20 +214,23 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a)
         if constexpr (IDX) tok = min(max(idx[min(tile * kTile + (lane & 31), vis.nv - 1)], 0), a.n - 1);
         return tok;
     };
-    TileRegs<KT> regs;
-    int tok = 0;
-    if (t < t1) {
-        load_tile<KT, IDX>(a, b, g, vis, t * kTile, list_tokens(t), regs);
-        tok = list_tokens(min(t + 4, t1 - 1));
-    }
-    for (; t < t1; t += 4) {
+    constexpr int kAhead = kTilesAhead<KT>;
+    TileRegs<KT> regs[kAhead];
+    int tok[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (t + 4 * u < t1) {
+            load_tile<KT, IDX>(a, b, g, vis, (t + 4 * u) * kTile, list_tokens(t + 4 * u), regs[u]);
+            tok[u] = list_tokens(min(t + 4 * (u + kAhead), t1 - 1));
+        }
+    auto step = [&](int t, TileRegs<KT>& regs, int& tok) {
         f32x4_v x[2];
         stage_values<KT>(regs, vl);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // other lanes read what this one wrote
         tile_logits<KT>(regs, qf, x);
-        if (t + 4 < t1) {
-            load_tile<KT, IDX>(a, b, g, vis, (t + 4) * kTile, tok, regs);
-            tok = list_tokens(min(t + 8, t1 - 1));
+        if (t + 4 * kAhead < t1) {
+            load_tile<KT, IDX>(a, b, g, vis, (t + 4 * kAhead) * kTile, tok, regs);
+            tok = list_tokens(min(t + 8 * kAhead, t1 - 1));
         }
         float p[8];
 #pragma unroll
@@ -266,6 +273,11 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
             for (int u = 0; u < kTerms; ++u) o[d] = mfma16<DT>(vf, pt[u], o[d]);
         }
+    };
+    for (; t < t1; t += 4 * kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (t + 4 * u < t1) step(t + 4 * u, regs[u], tok[u]);
     }
 
     // the four waves' outputs: (m, l) first, then the weighted sums

@@ -5,8 +5,8 @@
 // takes kEvictChunk result rows of one (sequence, KV head): it reads their
 // sources into registers, says so in a flag, waits until every chunk whose
 // sources lie in its own destination rows has said so, and writes.  Those are
-// chunks before it (a source never lies before its destination), and chunks are
-// handed out by a counter in ascending order, so every chunk waited for is held by a
+// chunks before it (a source never lies before its destination), and a group's chunks are
+// handed out by its counter in ascending order, so every chunk waited for is held by a
 // workgroup that runs or has ended and sets its flag without waiting: each
 // wait ends.  Each kept row is read once and written once; the bound is a copy's.
 #include "hill_device.h"
@@ -31,14 +31,16 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a)
     __shared__ int32_t src[kEvictChunk];
     __shared__ int ticket;
     const int tid = threadIdx.x;
-    if (tid == 0) ticket = (int)atomicAdd(a.flags, 1u);
-    __syncthreads();
     const int groups = a.B * a.heads;
-    if ((unsigned)ticket >= gridDim.x) return;               // only where two calls share a workspace
-    const int c = ticket / groups, bg = ticket % groups;     // chunk by chunk over all groups
+    const int bg = blockIdx.x % groups;
+    uint32_t* flags = a.flags + (int64_t)bg * a.flag_words;
+    if (tid == 0) ticket = (int)atomicAdd(flags, 1u);
+    ++flags;
+    __syncthreads();
+    const int c = ticket;
+    if ((unsigned)c >= (unsigned)a.chunks) return;           // only where two calls share a workspace
     const int b = bg / a.heads, g = bg % a.heads;
     const int r = a.R > 1 ? g : 0;
-    uint32_t* flags = a.flags + 1 + (int64_t)bg * a.chunks;
     const int32_t* idx = a.idx + ((int64_t)b * a.R + r) * a.keep;
     const int d0 = c * kEvictChunk, cnt = min(kEvictChunk, a.keep - d0);
     if (tid < kEvictChunk) src[tid] = min(max(idx[d0 + min(tid, cnt - 1)], 0), a.n - 1);
@@ -46,7 +48,7 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a)
     const bool own_s = a.R > 1 || g == 0;                    // this group moves the row's S and positions
     const bool moves = src[cnt - 1] != d0 + cnt - 1;         // ascending: else no row of the chunk moves
     float* srow = a.s + (int64_t)b * a.s_sb + (int64_t)r * a.s_sr;
-    int32_t* prow = a.pos ? a.pos + (int64_t)b * a.s_sb + (int64_t)r * a.s_sr : nullptr;
+    int32_t* prow = a.pos ? a.pos + (int64_t)b * a.p_sb + (int64_t)r * a.p_sr : nullptr;
 
     float sv = 0.0f;
     int32_t pv = 0;

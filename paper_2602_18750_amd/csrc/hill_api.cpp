@@ -737,7 +737,7 @@ int64_t evict_chunks(int k_keep) { return (k_keep + kEvictChunk - 1) / kEvictChu
 size_t evict_bytes(const Shape& s, int k_keep, size_t* flags)
 {
     *flags = layout_for(evict_shape(s), k_keep).end_topk;
-    return *flags + align256((1 + (size_t)s.B * s.Hkv * evict_chunks(k_keep)) * sizeof(uint32_t));
+    return *flags + align256((size_t)s.B * s.Hkv * evict_flag_words(evict_chunks(k_keep)) * sizeof(uint32_t));
 }
 
 }  // namespace
@@ -1069,7 +1069,8 @@ hill_status hill_evict_workspace_bytes(const hill_desc* d, int32_t k_keep, size_
 }
 
 hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t* idx_out, void* k, void* v,
-                       const hill_packed* p, int32_t* pos, void* ws, size_t ws_bytes, void* stream)
+                       const hill_packed* p, int32_t* pos, int64_t pos_stride_b, int64_t pos_stride_r, void* ws,
+                       size_t ws_bytes, void* stream)
 {
     Shape s;
     HILL_TRY(check_desc(d, &s));
@@ -1078,6 +1079,8 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     HILL_TRY(check_ptr(s_acc, "s"));
     if (!idx_out || ((uintptr_t)idx_out & 3u)) return fail(HILL_ERR_INVALID_ARG, "idx_out is NULL or not 4-byte aligned");
     if ((uintptr_t)pos & 3u) return fail(HILL_ERR_INVALID_ARG, "pos is not 4-byte aligned");
+    if (pos && ((s.R > 1 && pos_stride_r < s.n) || (s.B > 1 && pos_stride_b < (s.R - 1) * pos_stride_r + s.n)))
+        return fail(HILL_ERR_INVALID_ARG, "rows of pos overlap");
     if (!k != !v) return fail(HILL_ERR_INVALID_ARG, "k and v go together");
     if (k && p) return fail(HILL_ERR_INVALID_ARG, "k and v, or a packed cache, not both");
     if (k) {
@@ -1098,7 +1101,8 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     const Layout L = layout_for(evict_shape(s), k_keep);
     EvictArgs a{};
     a.flags = at<uint32_t>(ws, flags);
-    HIP_TRY(launch_fill_zero(a.flags, 1 + s.B * heads * chunks, st));
+    a.flag_words = evict_flag_words(chunks);
+    HIP_TRY(launch_fill_zero(a.flags, s.B * heads * a.flag_words, st));
     HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st));
     a.idx = idx_out;
     a.B = s.B;
@@ -1108,6 +1112,8 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     a.keep = k_keep;
     a.s = s_acc;
     a.pos = pos;
+    a.p_sb = pos_stride_b;
+    a.p_sr = pos_stride_r;
     a.s_sb = d->s_stride_b;
     a.s_sr = d->s_stride_r;
     a.k = static_cast<uint16_t*>(k);

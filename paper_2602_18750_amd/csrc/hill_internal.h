@@ -470,8 +470,8 @@ struct EvictArgs {
     const int32_t* idx;       // [B,R,keep] ascending
     int B, R, Hkv, n, keep;
     float* s;
-    int32_t* pos;             // nullable, strides of s
-    int64_t s_sb, s_sr;
+    int32_t* pos;             // nullable
+    int64_t s_sb, s_sr, p_sb, p_sr;
     uint16_t* k;              // nullable, with v
     uint16_t* v;
     int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
@@ -480,11 +480,15 @@ struct EvictArgs {
     uint32_t* kp;
     uint32_t* vp;
     int64_t cap;
-    uint32_t* flags;          // [1 + B * heads * chunks]: a ticket counter, then chunks whose sources have been read; zeroed
+    uint32_t* flags;          // [B * heads, flag_words]: a group's ticket counter, then its chunks whose sources have
+                              //   been read; zeroed
+    int64_t flag_words;
     int heads;                // row groups per sequence that move: Hkv, or R without K and V
     int chunks;
 };
 constexpr int kEvictChunk = 64;   // kept rows per workgroup
+// Words of a group's counter and flags: whole 128-byte lines, so that the groups' counters do not share one.
+inline int64_t evict_flag_words(int64_t chunks) { return (1 + chunks + 31) / 32 * 32; }
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
 
 hipError_t launch_attn_split(const AttnArgs& a, int dtype, hipStream_t st);

@@ -49,7 +49,7 @@ __device__ __forceinline__ f32x16_v mfma32(uint4 a, uint4 b, f32x16_v c)
 __device__ __forceinline__ u32x2_v read_transposed(const uint16_t* p)
 {
     typedef __attribute__((address_space(3))) short4_v* lds_ptr;
-    return __builtin_bit_cast(u32x2_v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)p));
+    return __builtin_bit_cast(u32x2_v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p));
 }
 
 // Softmax weights are split exactly enough for the 32-bit result: bf16 terms

@@ -54,7 +54,9 @@ __device__ __forceinline__ void load_lds16(const uint16_t* from, uint16_t* to)
 template <int DT>
 __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][kTileHalfs];   // [buffer][K, V]
+    // four arrays of their own, each step's named at compile time: the compiler then knows that the direct loads into one
+    // pair do not write what is read from the other, and does not wait for them before the first read
+    __shared__ __attribute__((aligned(16))) uint16_t k0[kTileHalfs], v0[kTileHalfs], k1[kTileHalfs], v1[kTileHalfs];
     const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hf = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (sequence, KV head) fastest, so that its blocks meet its K and V in one L2; the last tokens, whose windows
@@ -90,10 +92,8 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
         const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh;
         auto tile_begin = [&](int t) { return t < st ? t * kKeys : ws + (t - st) * kKeys; };
         auto tile_end = [&](int t) { return t < st ? min(ns, (t + 1) * kKeys) : min(pb + 1, ws + (t - st + 1) * kKeys); };
-        auto load = [&](int t) {   // rows past the tile's end repeat its last one (they weigh 0)
+        auto load = [&](int t, uint16_t* kl, uint16_t* vl) {   // rows past the tile's end repeat its last one (they weigh 0)
             const int j0 = tile_begin(t), jl = tile_end(t) - 1;
-            uint16_t* kl = lds[t & 1][0];
-            uint16_t* vl = lds[t & 1][1];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int jr = 16 * u + 4 * w + (lane >> 4);
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
                 load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + (16 * u + 4 * w) * kHeadDim);
             }
         };
-        load(0);
+        load(0, k0, v0);
         uint4 qf[8];
         const float s2 = fabsf(a.s2);                   // a negative scale goes into the query's signs
         const uint32_t flip = a.s2 < 0.0f ? 0x80008000u : 0u;
@@ -116,15 +116,13 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
 
         // this lane's LDS offsets (elements): K piece (2i + hf) of row c32 (+ 32), V rows 4 hf + (c16 / 4) on
         const int c16 = lane & 15, vrow = 4 * hf + (c16 >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((c16 & 3) >> 1);
-        for (int t = 0; t < nt; ++t) {
+        auto step = [&](int t, const uint16_t* kl, const uint16_t* vl, uint16_t* kn, uint16_t* vn) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();       // tile t is there, and every wave has left tile t - 1
-            if (t + 1 < nt) load(t + 1);
+            if (t + 1 < nt) load(t + 1, kn, vn);
             const int j0 = tile_begin(t), j1 = tile_end(t);
             // nothing of the tile visible to this wave's rows
-            if (j0 > pw1 || (j0 >= a.sink && j1 - 1 <= pw0 - a.window)) continue;
-            const uint16_t* kl = lds[t & 1][0];
-            const uint16_t* vl = lds[t & 1][1];
+            if (j0 > pw1 || (j0 >= a.sink && j1 - 1 <= pw0 - a.window)) return;
             f32x16_v x[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -193,6 +191,10 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
                     o[d] = mfma32<DT>(make_uint4(lo.x, lo.y, hi.x, hi.y), pf[q], o[d]);
                 }
             }
+        };
+        for (int t = 0; t < nt; t += 2) {
+            step(t, k0, v0, k1, v1);
+            if (t + 1 < nt) step(t + 1, k1, v1, k0, v0);
         }
     }
     l += __shfl_xor(l, 32, 64);

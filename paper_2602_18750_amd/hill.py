@@ -202,7 +202,7 @@ def load_library(path: str = LIB_PATH):
                            ("hill_packed_workspace_bytes", [D, I32, I32, SZP]),
                            ("hill_packed_attn", [D, K, P, P, P, I32, P, P, P, SZ, P]),
                            ("hill_evict_workspace_bytes", [D, I32, SZP]),
-                           ("hill_evict", [D, P, I32, P, P, P, K, P, P, SZ, P])):
+                           ("hill_evict", [D, P, I32, P, P, P, K, P, ctypes.c_int64, ctypes.c_int64, P, SZ, P])):
             getattr(lib, name).argtypes = args
             getattr(lib, name).restype = ctypes.c_int
         if lib.hill_abi_version() != ABI_VERSION:
