@@ -41,46 +41,108 @@ struct TileRegs {
     uint32_t kp[2], vp[2];       // packed: (scale, zero) of the codes above
 };
 
-// Tiles that a wave requests ahead of the one it works on.
+// Where the rows of a tile lie: bases of the (sequence, KV head) for every lane,
+// and each lane's offsets from a tile's first row, which are the same in every
+// tile of consecutive tokens.
 template <int KT>
-constexpr int kTilesAhead = KT == kRowsPacked ? 2 : 1;
+struct RowBase {
+    const char* k;
+    const char* v;
+    const char* kp;
+    const char* vp;
+    uint32_t ko, vo;                                // bytes from the tile's first row
+    bool near;                                      // the offsets fit 32 bits
+};
 
-// Tokens are taken into [0, n), so that a bad list entry reads a valid row.
+template <int KT>
+__device__ __forceinline__ RowBase<KT> row_base(const CacheAttnArgs& a, int b, int g)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, qd = lane >> 4;
+    RowBase<KT> r;
+    if constexpr (KT == kRowsPacked) {
+        const int64_t row0 = ((int64_t)b * a.Hkv + g) * a.cap;
+        r.k = reinterpret_cast<const char*>(a.kc) + row0 * 64;
+        r.v = reinterpret_cast<const char*>(a.vc) + row0 * 64;
+        r.kp = reinterpret_cast<const char*>(a.kp) + row0 * 16;
+        r.vp = reinterpret_cast<const char*>(a.vp) + row0 * 16;
+        r.ko = c * 64 + qd * 16;
+        r.vo = lane * 16;
+        r.near = true;
+    } else {
+        r.k = reinterpret_cast<const char*>(a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh);
+        r.v = reinterpret_cast<const char*>(a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh);
+        r.ko = c * 2 * (uint32_t)a.k_sn + qd * 16;
+        r.vo = qd * 2 * (uint32_t)a.v_sn + c * 16;
+        r.near = max(a.k_sn, a.v_sn) < (1 << 25);
+    }
+    return r;
+}
+
+__device__ __forceinline__ uint32_t load_word(const char* p) { return *reinterpret_cast<const uint32_t*>(p); }
+
+// Positions [i0, i0 + 32): consecutive tokens from uniform bases, or (at the
+// ends of the visible ranges, and over lists) a token per row; positions past
+// the last repeat it.  tok: a list's tokens, taken into [0, n).
 template <int KT, bool IDX>
-__device__ __forceinline__ void load_tile(const CacheAttnArgs& a, int b, int g, const Visible& vis, int i0, int tok,
+__device__ __forceinline__ void load_tile(const CacheAttnArgs& a, const RowBase<KT>& r, const Visible& vis, int i0, int tok,
                                           TileRegs<KT>& t)
 {
     const int lane = threadIdx.x & 63, c = lane & 15, qd = lane >> 4;
-    auto token = [&](int i) {   // of position i0 + i, the last one repeated
-        if constexpr (IDX) return __shfl(tok, i, 64);
-        return vis.token(min(i0 + i, vis.nv - 1));
+    // One branch on one value: as a chain of conditions the compiler joined the paths with registers that one of
+    // them had not set.
+    const bool plain = !IDX & r.near & (i0 + kTile <= vis.nv) & ((i0 >= vis.ns) | (i0 + kTile <= vis.ns));
+    if (plain) {
+        const uint64_t j0 = (uint64_t)vis.token(i0);
+        if constexpr (KT == kRowsPacked) {
+            const char *k = r.k + j0 * 64, *v = r.v + j0 * 64, *kp = r.kp + j0 * 16, *vp = r.vp + j0 * 16;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                t.k[u] = load_stream16(k + r.ko + 1024 * u);
+                t.kp[u] = load_word(kp + (r.ko >> 2) + 256 * u);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                t.v[u] = load_stream16(v + r.vo + 1024 * u);
+                t.vp[u] = load_word(vp + (r.vo >> 2) + 256 * u);
+            }
+        } else {
+            const uint64_t kn = 2 * (uint64_t)(uint32_t)a.k_sn, vn = 2 * (uint64_t)(uint32_t)a.v_sn;
+            const char *k = r.k + j0 * kn, *v = r.v + j0 * vn;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t.k[4 * u + i] = load_stream16(k + 16 * u * kn + r.ko + 64 * i);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t.v[u] = load_stream16(v + 4 * u * vn + r.vo);
+        }
+        return;
+    }
+    auto token = [&](int i) -> uint64_t {   // of position i0 + i
+        if constexpr (IDX) return (uint64_t)__shfl(tok, i, 64);
+        return (uint64_t)vis.token(min(i0 + i, vis.nv - 1));
     };
     if constexpr (KT == kRowsPacked) {
-        const int64_t row0 = ((int64_t)b * a.Hkv + g) * a.cap;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t row = row0 + token(16 * u + c);
-            t.k[u] = *reinterpret_cast<const uint4*>(a.kc + row * 64 + qd * 16);
-            t.kp[u] = a.kp[row * 4 + qd];
+            const uint32_t at = 64u * (uint32_t)token(16 * u + c) + 16u * qd;   // n < 2^22
+            t.k[u] = load_stream16(r.k + at);
+            t.kp[u] = load_word(r.kp + (at >> 2));
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t row = row0 + token(16 * u + (lane >> 2));
-            t.v[u] = *reinterpret_cast<const uint4*>(a.vc + row * 64 + (lane & 3) * 16);
-            t.vp[u] = a.vp[row * 4 + (lane & 3)];
+            const uint32_t at = 64u * (uint32_t)token(16 * u + (lane >> 2)) + 16u * (lane & 3);
+            t.v[u] = load_stream16(r.v + at);
+            t.vp[u] = load_word(r.vp + (at >> 2));
         }
     } else {
-        const uint16_t* kb = a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh + qd * 8;
-        const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh + c * 8;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint16_t* r = kb + (uint64_t)(uint32_t)token(16 * u + c) * (uint32_t)a.k_sn;
+            const char* k = r.k + token(16 * u + c) * 2 * (uint32_t)a.k_sn + 16 * qd;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t.k[4 * u + i] = *reinterpret_cast<const uint4*>(r + 32 * i);
+            for (int i = 0; i < 4; ++i) t.k[4 * u + i] = load_stream16(k + 64 * i);
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            t.v[u] = *reinterpret_cast<const uint4*>(vb + (uint64_t)(uint32_t)token(4 * u + qd) * (uint32_t)a.v_sn);
+        for (int u = 0; u < 8; ++u) t.v[u] = load_stream16(r.v + token(4 * u + qd) * 2 * (uint32_t)a.v_sn + 16 * c);
     }
 }
 
@@ -161,7 +223,7 @@ __device__ __forceinline__ float bf16_query_to_half(uint4 (&qf)[4])
 }
 
 template <int KT, bool IDX, bool LOG>
-__global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
+__global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_kernel(CacheAttnArgs a)
 {
     constexpr int DT = KT == kRowsBf16 ? 1 : 0;
     constexpr int kTerms = kWeightTerms<DT>;
@@ -191,14 +253,13 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
     int t = split * per + w;
 
     uint4 qf[4];
-    float s2 = a.s2;
+    float s2 = fabsf(a.s2);                            // a negative scale goes into the query's signs
+    const uint32_t flip = a.s2 < 0.0f ? 0x80008000u : 0u;
     {
         const uint16_t* qr = a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             qf[i] = *reinterpret_cast<const uint4*>(qr + (KT == kRowsPacked ? 32 * qd + 8 * i : 32 * i + 8 * qd));
-        if constexpr (KT == kRowsPacked)
-            if (a.q_bf16) s2 *= bf16_query_to_half(qf);
     }
 
     uint16_t* vl = vlds + w * kTile * kVRow;
@@ -214,27 +275,29 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
         if constexpr (IDX) tok = min(max(idx[min(tile * kTile + (lane & 31), vis.nv - 1)], 0), a.n - 1);
         return tok;
     };
-    constexpr int kAhead = kTilesAhead<KT>;
-    TileRegs<KT> regs[kAhead];
-    int tok[kAhead];
+    const RowBase<KT> base = row_base<KT>(a, b, g);
+    TileRegs<KT> regs;
+    int tok = 0;
+    if (t < t1) {
+        load_tile<KT, IDX>(a, base, vis, t * kTile, list_tokens(t), regs);
+        tok = list_tokens(min(t + 4, t1 - 1));
+    }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-        if (t + 4 * u < t1) {
-            load_tile<KT, IDX>(a, b, g, vis, (t + 4 * u) * kTile, list_tokens(t + 4 * u), regs[u]);
-            tok[u] = list_tokens(min(t + 4 * (u + kAhead), t1 - 1));
-        }
-    auto step = [&](int t, TileRegs<KT>& regs, int& tok) {
+    for (int i = 0; i < 4; ++i) qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
+    if constexpr (KT == kRowsPacked)   // with the first rows on their way
+        if (a.q_bf16) s2 *= bf16_query_to_half(qf);
+    for (; t < t1; t += 4) {
         f32x4_v x[2];
         stage_values<KT>(regs, vl);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // other lanes read what this one wrote
         tile_logits<KT>(regs, qf, x);
-        if (t + 4 * kAhead < t1) {
-            load_tile<KT, IDX>(a, b, g, vis, (t + 4 * kAhead) * kTile, tok, regs);
-            tok = list_tokens(min(t + 8 * kAhead, t1 - 1));
+        if (t + 4 < t1) {
+            load_tile<KT, IDX>(a, base, vis, (t + 4) * kTile, tok, regs);
+            tok = list_tokens(min(t + 8, t1 - 1));
         }
         float p[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = x[e >> 2][e & 3] * s2;
+        for (int e = 0; e < 8; ++e) p[e] = x[e >> 2][e & 3];
         const int i0 = t * kTile + 4 * qd;             // this lane's positions: i0 + r and i0 + 16 + r
         if ((t + 1) * kTile > vis.nv) {
 #pragma unroll
@@ -244,14 +307,14 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
         if constexpr (LOG) {
             if (h0 + c < a.G) {
                 float* to = a.logits + ((int64_t)b * a.Hq + h) * a.ld + i0;   // ld holds whole tiles
-                *reinterpret_cast<float4*>(to) = make_float4(p[0], p[1], p[2], p[3]);
-                *reinterpret_cast<float4*>(to + 16) = make_float4(p[4], p[5], p[6], p[7]);
+                *reinterpret_cast<float4*>(to) = make_float4(p[0] * s2, p[1] * s2, p[2] * s2, p[3] * s2);
+                *reinterpret_cast<float4*>(to + 16) = make_float4(p[4] * s2, p[5] * s2, p[6] * s2, p[7] * s2);
             }
         }
         float mx = p[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, p[e]);
-        const float m_new = fmaxf(m, max_x16_x32(mx));
+        const float m_new = fmaxf(m, max_x16_x32(mx) * s2);
         if (__any(m_new > m)) {
             const float al = exp2_ftz(m - m_new);
             l *= al;
@@ -259,9 +322,10 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
             for (int d = 0; d < 8; ++d) o[d] *= al;
         }
         m = m_new;
+        const float ref = m - kWeightShift<DT>;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            p[e] = exp2_ftz(p[e] - m + kWeightShift<DT>);
+            p[e] = exp2_ftz(__builtin_fmaf(p[e], s2, -ref));
             l += p[e];
         }
         uint4 pt[kTerms];
@@ -273,11 +337,6 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
 #pragma unroll
             for (int u = 0; u < kTerms; ++u) o[d] = mfma16<DT>(vf, pt[u], o[d]);
         }
-    };
-    for (; t < t1; t += 4 * kAhead) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (t + 4 * u < t1) step(t + 4 * u, regs[u], tok[u]);
     }
 
     // the four waves' outputs: (m, l) first, then the weighted sums
@@ -291,16 +350,18 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
     for (int u = 0; u < 4; ++u) L += ml[u][c].y > 0.0f ? ml[u][c].y * exp2_ftz(ml[u][c].x - M) : 0.0f;
     const float mine = l > 0.0f ? exp2_ftz(m - M) : 0.0f;
     float* ol = reinterpret_cast<float*>(vlds);        // [4][kHeads][kHeadDim]
+    const int heads = min(kHeads, a.G - h0);
+    if (c < heads) {
 #pragma unroll
-    for (int d = 0; d < 8; ++d)
-        *reinterpret_cast<f32x4_v*>(ol + (w * kHeads + c) * kHeadDim + 16 * d + 4 * qd) = o[d] * mine;
+        for (int d = 0; d < 8; ++d)
+            *reinterpret_cast<f32x4_v*>(ol + (w * kHeads + c) * kHeadDim + 16 * d + 4 * qd) = o[d] * mine;
+    }
     if (tid < kHeads) {                                // lane c of wave 0 holds head c
         inv_l[tid] = L > 0.0f ? 1.0f / L : 0.0f;       // nothing visible: 0
         if (a.part_ml && h0 + tid < a.G)
             a.part_ml[((int64_t)b * a.Hq + g * a.G + h0 + tid) * a.nsplit + split] = make_float2(M, L);
     }
     __syncthreads();
-    const int heads = min(kHeads, a.G - h0);
     for (int e = tid; e < heads * (kHeadDim / 4); e += 256) {
         const int hh = e / (kHeadDim / 4), d = e % (kHeadDim / 4) * 4;
         f32x4_v s = *reinterpret_cast<const f32x4_v*>(ol + hh * kHeadDim + d);
@@ -312,31 +373,63 @@ __global__ __launch_bounds__(256, 3) void cache_attn_kernel(CacheAttnArgs a)
     }
 }
 
-// One share per thread of a head at most (kMaxCacheSplits); empty shares have
-// l = 0, and a head without any l gives 0.
-__device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t bh, float* red, float* wgt, float* osum)
+// Joins the shares of 8 / NG heads per workgroup: 32 lanes a head and share
+// group, four dimensions each; group i of NG takes shares i, i + NG, ... with all their
+// loads in flight (up to eight at a time).  Empty shares have l = 0, and a head without any l gives 0.
+template <int NG>
+__device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t block, f32x4_v* osum, float2* mlsum)
 {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    float2 v = make_float2(-INFINITY, 0.0f);
-    if (tid < a.nsplit) v = a.part_ml[bh * a.nsplit + tid];
-    const float mx = wave_max(v.y > 0.0f ? v.x : -INFINITY);
-    if (lane == 0) red[w] = mx;
-    __syncthreads();
-    const float M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float x = v.y > 0.0f ? exp2_ftz(v.x - M) : 0.0f;
-    wgt[tid] = x;
-    const float ls = wave_sum(x * v.y);
-    if (lane == 0) red[4 + w] = ls;
-    __syncthreads();
-    const float L = (red[4] + red[5]) + (red[6] + red[7]);
-    const int d = tid & (kHeadDim - 1), half = tid / kHeadDim;
+    const int tid = threadIdx.x, grp = (tid >> 5) % NG, d = 4 * (tid & 31);
+    const int64_t heads = (int64_t)a.B * a.Hq, mine = block * (8 / NG) + (tid >> 5) / NG;
+    const int64_t bh = mine < heads ? mine : heads - 1;     // past the last: it again, not stored
+    const float2* ml = a.part_ml + bh * a.nsplit;
     const float* po = a.part_o + bh * a.nsplit * kHeadDim + d;
-    float o = 0.0f;
-#pragma unroll 8
-    for (int s = half; s < a.nsplit; s += 2) o += wgt[s] * po[(int64_t)s * kHeadDim];
-    osum[tid] = o;
-    __syncthreads();
-    if (half == 0) a.out[bh * kHeadDim + d] = L > 0.0f ? (o + osum[tid + kHeadDim]) / L : 0.0f;
+    float m = -INFINITY, l = 0.0f;
+    f32x4_v o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = grp; s0 < a.nsplit; s0 += 8 * NG) {
+        float2 v[8];
+        f32x4_v x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                       // past the last share: it again, with weight 0
+            const int s = min(s0 + i * NG, a.nsplit - 1);
+            v[i] = ml[s];
+            x[i] = *reinterpret_cast<const f32x4_v*>(po + (int64_t)s * kHeadDim);
+            if (s0 + i * NG >= a.nsplit) v[i].y = 0.0f;
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].y > 0.0f ? v[i].x : -INFINITY);
+        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
+        o *= al;
+        l *= al;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = v[i].y > 0.0f ? exp2_ftz(v[i].x - top) : 0.0f;
+            o += f * x[i];
+            l += f * v[i].y;
+        }
+        m = top;
+    }
+    if constexpr (NG > 1) {
+        osum[tid] = o;
+        mlsum[tid] = make_float2(m, l);
+        __syncthreads();
+        if (grp != 0) return;
+        float top = m;
+#pragma unroll
+        for (int i = 1; i < NG; ++i) top = fmaxf(top, mlsum[tid + 32 * i].x);
+        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
+        o *= al;
+        l *= al;
+#pragma unroll
+        for (int i = 1; i < NG; ++i) {
+            const float2 v = mlsum[tid + 32 * i];
+            const float f = v.y > 0.0f ? exp2_ftz(v.x - top) : 0.0f;
+            o += f * osum[tid + 32 * i];
+            l += f * v.y;
+        }
+    }
+    if (mine < heads) *reinterpret_cast<f32x4_v*>(a.out + bh * kHeadDim + d) = l > 0.0f ? o * (1.0f / l) : o * 0.0f;
 }
 
 // S[b, r, j(i)] += the weights of the row's heads, 1024 positions per workgroup:
@@ -402,16 +495,14 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t bloc
         if (i + u < vis.nv) s[vis.token(i + u)] += e[u];
 }
 
-// The first merge_blocks workgroups join one head's shares each, the others add weights.
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a, int64_t merge_blocks)
+// The first merge_blocks workgroups join shares, the others add weights.
+template <int NG>
+__global__ __launch_bounds__(256, 4) void cache_merge_kernel(CacheAttnArgs a, int64_t merge_blocks)
 {
-    __shared__ float2 red[256];
-    __shared__ float2 stat[256];
-    if ((int64_t)blockIdx.x < merge_blocks)
-        merge_shares(a, blockIdx.x, reinterpret_cast<float*>(stat), reinterpret_cast<float*>(red),
-                     reinterpret_cast<float*>(red) + 256);
-    else
-        add_weights(a, (int64_t)blockIdx.x - merge_blocks, red, stat);
+    __shared__ f32x4_v buf[256 + 128];
+    float2* two = reinterpret_cast<float2*>(buf + 256);
+    if ((int64_t)blockIdx.x < merge_blocks) merge_shares<NG>(a, blockIdx.x, buf, two);
+    else add_weights(a, (int64_t)blockIdx.x - merge_blocks, two, reinterpret_cast<float2*>(buf));
 }
 
 template <int KT>
@@ -435,9 +526,14 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st)
     else if (dtype == 1) launch_rows<kRowsBf16>(a, st);
     else launch_rows<kRowsF16>(a, st);
     if (hipError_t e = hipGetLastError()) return e;
-    const int64_t merge = a.nsplit > 1 ? (int64_t)a.B * a.Hq : 0, add = a.s ? (int64_t)a.B * a.R * a.s_chunks : 0;
+    // few shares: eight heads a workgroup; many: one head, its shares over eight groups
+    const bool few = a.nsplit <= 8;
+    const int64_t bh = (int64_t)a.B * a.Hq;
+    const int64_t merge = a.nsplit > 1 ? (few ? (bh + 7) / 8 : bh) : 0, add = a.s ? (int64_t)a.B * a.R * a.s_chunks : 0;
     if (merge + add == 0) return hipSuccess;
-    hipLaunchKernelGGL(cache_merge_kernel, dim3((unsigned)(merge + add)), dim3(256), 0, st, a, merge);
+    const dim3 grid((unsigned)(merge + add));
+    if (few) hipLaunchKernelGGL(cache_merge_kernel<1>, grid, dim3(256), 0, st, a, merge);
+    else hipLaunchKernelGGL(cache_merge_kernel<8>, grid, dim3(256), 0, st, a, merge);
     return hipGetLastError();
 }
 

@@ -889,7 +889,7 @@ hill_status hill_window_attn(const hill_desc* d, const void* q, const void* k, c
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
     const CacheLayout L = cache_layout(d, s, 0, false);
-    HILL_TRY(check_grid(L.wgs));
+    HILL_TRY(check_grid(L.wgs + (int64_t)s.B * s.Hq));
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
     a.k = static_cast<const uint16_t*>(k);

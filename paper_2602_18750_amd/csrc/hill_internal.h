@@ -420,15 +420,15 @@ struct CacheAttnArgs {
     int64_t ld;
     int s_chunks;             //   kScoreChunk-position chunks per row
 };
-constexpr int kMaxCacheSplits = 256;   // one per thread of the merge
 constexpr int kScoreChunk = 1024;
-// Shares of `seen` visible positions: until about three workgroups per CU run
-// (of 256), each of at least four 32-token tiles, one per wave.
+// Shares of `seen` visible positions: one where (sequence, KV head) pairs alone
+// give every CU a workgroup (of 256), so that nothing is left to join; else
+// about two workgroups per CU, each of at least four 32-token tiles, one per wave.
 inline int cache_splits(int64_t wgs, int64_t seen)
 {
-    const int64_t want = (768 + wgs - 1) / wgs, most = (seen + 127) / 128;
+    const int64_t want = wgs >= 256 ? 1 : (512 + wgs / 2) / wgs, most = (seen + 127) / 128;
     const int64_t s = want < most ? want : most;
-    return s < 1 ? 1 : s > kMaxCacheSplits ? kMaxCacheSplits : (int)s;
+    return s < 1 ? 1 : (int)s;
 }
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
 

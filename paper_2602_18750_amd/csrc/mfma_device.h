@@ -10,6 +10,7 @@ namespace hill {
 
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf168_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_v __attribute__((ext_vector_type(2)));
 typedef float f32x4_v __attribute__((ext_vector_type(4)));
 typedef float f32x16_v __attribute__((ext_vector_type(16)));
 typedef short short4_v __attribute__((ext_vector_type(4)));
@@ -84,8 +85,9 @@ __device__ __forceinline__ void split_weights(const float (&p)[8], uint4 (&t)[kW
                 y -= __uint_as_float(yb & 0xffff0000u);
             }
         } else {
-            const half2_t h = {(_Float16)x, (_Float16)y};
-            const half2_t r = {(_Float16)(x - (float)h[0]), (_Float16)(y - (float)h[1])};
+            const half2_t h = __builtin_convertvector(f32x2_v{x, y}, half2_t);
+            const half2_t r = __builtin_convertvector((f32x2_v{__builtin_fmaf((float)h[0], -1.0f, x), __builtin_fmaf((float)h[1], -1.0f, y)}),
+                                                      half2_t);
             w[0][i] = __builtin_bit_cast(uint32_t, h);
             w[1][i] = __builtin_bit_cast(uint32_t, r);
         }
@@ -102,12 +104,14 @@ __device__ __forceinline__ uint4 decode8(uint32_t x, half2_t scale, half2_t zero
 {
     const half2_t k1024 = {(_Float16)1024.0f, (_Float16)1024.0f};
     const half2_t k16th = {(_Float16)0.0625f, (_Float16)0.0625f}, k64 = {(_Float16)-64.0f, (_Float16)-64.0f};
+    uint32_t exponent = 0x64006400u;
+    asm("" : "+v"(exponent));   // in a vector register: one v_and_or_b32 takes one constant
     uint32_t r[4];
 #pragma unroll
     for (int s = 0; s < 4; s += 2) {
         const uint32_t y = x >> (4 * s);
-        const half2_t lo = __builtin_bit_cast(half2_t, (y & 0x000f000fu) | 0x64006400u) - k1024;
-        const half2_t hi = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (y & 0x00f000f0u) | 0x64006400u), k16th, k64);
+        const half2_t lo = __builtin_bit_cast(half2_t, (y & 0x000f000fu) | exponent) - k1024;
+        const half2_t hi = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (y & 0x00f000f0u) | exponent), k16th, k64);
         r[s] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(lo, scale, zero));
         r[s + 1] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(hi, scale, zero));
     }

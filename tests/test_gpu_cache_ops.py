@@ -71,6 +71,44 @@ def test_window_attn(case, dtype):
     check_decode(out, q, k, v, lens or [n] * B, sink, window)
 
 
+def plain_decode(q, k, v, lens, sink, window):
+    """64-bit decode on the GPU, all rows at once: q [B, Hq, D], k, v [B, Hkv, n, D]."""
+    B, Hq, _ = q.shape
+    Hkv, n = k.shape[1], k.shape[2]
+    j = torch.arange(n, device=DEV)
+    m = torch.as_tensor(lens, device=DEV).view(B, 1)
+    seen = ((j < m) & ((j < sink) | (j >= m - window))).view(B, 1, 1, n)
+    x = torch.matmul(q.double().view(B, Hkv, Hq // Hkv, D), k.double().transpose(2, 3).contiguous()) * D ** -0.5
+    e = torch.where(seen, torch.exp(x - x.masked_fill(~seen, -1e300).amax(-1, keepdim=True)), torch.zeros_like(x))
+    w = e / e.sum(-1, keepdim=True)
+    return torch.matmul(w, v.double()).view(B, Hq, D), w
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("held", ["16-bit", "packed"])
+@pytest.mark.parametrize("sink,window", [(4, 700), (40, 612), (33, 900), (0, 0x7fffffff), (64, 64)])
+def test_many_tiles_per_wave(sink, window, held, dtype):
+    """Enough sequences that every wave walks several tiles: the first one across the sinks' end, the last one
+    partial, ragged lengths between."""
+    B, Hq, Hkv, n = 33, 16, 8, 1001
+    g = torch.Generator(device=DEV).manual_seed(sink + 7)
+    q = torch.randn((B, Hq, D), generator=g, device=DEV).to(dtype)
+    k, v = (torch.randn((B, Hkv, n, D), generator=g, device=DEV).to(dtype) for _ in range(2))
+    lens = torch.randint(1, n + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+    lens[0], lens[1], lens[2] = n, 1, 33
+    if held == "packed":
+        cache = H().pack_kv(k, v, H().new_packed_cache(B, Hkv, n, DEV))
+        out = H().hill_packed_attn(q, cache, lens=lens, n_sink=sink, window=window)
+        k, v = H().unpack_kv(cache)
+    else:
+        out = H().hill_window_attn(q, k, v, window=window, n_sink=sink, lens=lens)
+    want, w = plain_decode(q, k, v, lens, sink, window)
+    # as check_decode's bound, with the largest row's products for all and sum w |V| <= max |V|
+    size = torch.matmul(q.double().abs().view(B, Hkv, 2, D), k.double().abs().transpose(2, 3).contiguous()).amax(-1) * D ** -0.5
+    bound = (2 * (size * (D * R.F32 + 4 * R.F32 * 1.4427) + 8 * R.F32) + 2 * (n / 32 + 64) * R.F32).view(B, Hq, 1) * v.abs().max()
+    assert ((out.double() - want).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("scale", [0.0, 0.5, -0.2])
 def test_window_attn_strides_scales_and_unseen_rows(scale):
     """A [B, n, 2, Hkv, D] cache (K and V interleaved), more rows than tokens, a view of q, rows that no query sees
