@@ -157,10 +157,10 @@ __device__ __forceinline__ void stage_values(const TileRegs<KT>& t, uint16_t* vl
             half2_t scale, zero;
             group_params(t.vp[u], scale, zero);
             uint4* to = reinterpret_cast<uint4*>(vl + (16 * u + (lane >> 2)) * kVRow + (lane & 3) * 32);
-            to[0] = decode8(t.v[u].x, scale, zero);
-            to[1] = decode8(t.v[u].y, scale, zero);
-            to[2] = decode8(t.v[u].z, scale, zero);
-            to[3] = decode8(t.v[u].w, scale, zero);
+            to[0] = decode8_split(t.v[u].x, scale, zero);
+            to[1] = decode8_split(t.v[u].y, scale, zero);
+            to[2] = decode8_split(t.v[u].z, scale, zero);
+            to[3] = decode8_split(t.v[u].w, scale, zero);
         }
     } else {
 #pragma unroll
@@ -181,7 +181,7 @@ __device__ __forceinline__ void tile_logits(const TileRegs<KT>& t, const uint4 (
             group_params(t.kp[u], scale, zero);
             const uint32_t w[4] = {t.k[u].x, t.k[u].y, t.k[u].z, t.k[u].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[u] = mfma16<DT>(decode8(w[i], scale, zero), qf[i], x[u]);
+            for (int i = 0; i < 4; ++i) x[u] = mfma16<DT>(decode8_split(w[i], scale, zero), qf[i], x[u]);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[u] = mfma16<DT>(t.k[4 * u + i], qf[i], x[u]);
@@ -286,6 +286,12 @@ __global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_ker
     for (int i = 0; i < 4; ++i) qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
     if constexpr (KT == kRowsPacked)   // with the first rows on their way
         if (a.q_bf16) s2 *= bf16_query_to_half(qf);
+    if constexpr (KT == kRowsPacked) {   // the order in which decode8_split gives a key's elements
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            qf[i] = make_uint4(lower_halves(qf[i].x, qf[i].z), upper_halves(qf[i].x, qf[i].z),
+                               lower_halves(qf[i].y, qf[i].w), upper_halves(qf[i].y, qf[i].w));
+    }
     for (; t < t1; t += 4) {
         f32x4_v x[2];
         stage_values<KT>(regs, vl);
@@ -353,8 +359,16 @@ __global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_ker
     const int heads = min(kHeads, a.G - h0);
     if (c < heads) {
 #pragma unroll
-        for (int d = 0; d < 8; ++d)
-            *reinterpret_cast<f32x4_v*>(ol + (w * kHeads + c) * kHeadDim + 16 * d + 4 * qd) = o[d] * mine;
+        for (int d = 0; d < 8; ++d) {
+            const f32x4_v x = o[d] * mine;
+            if constexpr (KT == kRowsPacked) {   // a value's elements lie in decode8_split's order
+                float* to = ol + (w * kHeads + c) * kHeadDim + 16 * d + 8 * (qd >> 1) + 2 * (qd & 1);
+                *reinterpret_cast<f32x2_v*>(to) = f32x2_v{x[0], x[2]};
+                *reinterpret_cast<f32x2_v*>(to + 4) = f32x2_v{x[1], x[3]};
+            } else {
+                *reinterpret_cast<f32x4_v*>(ol + (w * kHeads + c) * kHeadDim + 16 * d + 4 * qd) = x;
+            }
+        }
     }
     if (tid < kHeads) {                                // lane c of wave 0 holds head c
         inv_l[tid] = L > 0.0f ? 1.0f / L : 0.0f;       // nothing visible: 0
@@ -373,15 +387,18 @@ __global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_ker
     }
 }
 
-// Joins the shares of 8 / NG heads per workgroup: 32 lanes a head and share
-// group, four dimensions each; group i of NG takes shares i, i + NG, ... with all their
-// loads in flight (up to eight at a time).  Empty shares have l = 0, and a head without any l gives 0.
-template <int NG>
+// Joins shares: LANES lanes of four dimensions each (32: a whole head) in NG
+// groups make a head, or a quarter of one; group i takes shares i, i + NG, ...
+// with up to eight loads in flight.  Empty shares have l = 0, and a head without any l gives 0.
+template <int NG, int LANES>
 __device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t block, f32x4_v* osum, float2* mlsum)
 {
-    const int tid = threadIdx.x, grp = (tid >> 5) % NG, d = 4 * (tid & 31);
-    const int64_t heads = (int64_t)a.B * a.Hq, mine = block * (8 / NG) + (tid >> 5) / NG;
-    const int64_t bh = mine < heads ? mine : heads - 1;     // past the last: it again, not stored
+    constexpr int kParts = 32 / LANES, kPerWg = 256 / (NG * LANES);   // parts of a head; (head, part) pairs per workgroup
+    const int tid = threadIdx.x, grp = tid / LANES % NG;
+    const int64_t pairs = (int64_t)a.B * a.Hq * kParts, mine = block * kPerWg + tid / (NG * LANES);
+    const int64_t bp = mine < pairs ? mine : pairs - 1;     // past the last: it again, not stored
+    const int64_t bh = bp / kParts;
+    const int d = 4 * (tid % LANES + LANES * (int)(bp % kParts));
     const float2* ml = a.part_ml + bh * a.nsplit;
     const float* po = a.part_o + bh * a.nsplit * kHeadDim + d;
     float m = -INFINITY, l = 0.0f;
@@ -416,25 +433,26 @@ __device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t blo
         __syncthreads();
         if (grp != 0) return;
         float top = m;
-#pragma unroll
-        for (int i = 1; i < NG; ++i) top = fmaxf(top, mlsum[tid + 32 * i].x);
+#pragma unroll 8
+        for (int i = 1; i < NG; ++i) top = fmaxf(top, mlsum[tid + LANES * i].x);
         const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
         o *= al;
         l *= al;
-#pragma unroll
+#pragma unroll 8
         for (int i = 1; i < NG; ++i) {
-            const float2 v = mlsum[tid + 32 * i];
+            const float2 v = mlsum[tid + LANES * i];
             const float f = v.y > 0.0f ? exp2_ftz(v.x - top) : 0.0f;
-            o += f * osum[tid + 32 * i];
+            o += f * osum[tid + LANES * i];
             l += f * v.y;
         }
     }
-    if (mine < heads) *reinterpret_cast<f32x4_v*>(a.out + bh * kHeadDim + d) = l > 0.0f ? o * (1.0f / l) : o * 0.0f;
+    if (mine < pairs) *reinterpret_cast<f32x4_v*>(a.out + bh * kHeadDim + d) = l > 0.0f ? o * (1.0f / l) : o * 0.0f;
 }
 
-// S[b, r, j(i)] += the weights of the row's heads, 1024 positions per workgroup:
-// the heads' (m, l) from the shares first, then each thread four positions of
-// every head, in head order.
+// S[b, r, j(i)] += the weights of the row's heads, 256 * SP positions per
+// workgroup: the heads' (m, l) from the shares first, then each thread SP
+// positions of every head, in head order.
+template <int SP>
 __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t block, float2* red, float2* stat)
 {
     const int tid = threadIdx.x;
@@ -444,8 +462,8 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t bloc
     const int heads = a.R > 1 ? a.G : a.Hq;
     const int64_t bh0 = (int64_t)b * a.Hq + (int64_t)r * a.G;
     const Visible vis = visible(seq_len(a.lens, b, a.n), a.sink, a.window);
-    const int i = chunk * kScoreChunk + 4 * tid;
-    if (chunk * kScoreChunk >= vis.nv) return;           // the same for the whole workgroup
+    const int i = chunk * 256 * SP + SP * tid;
+    if (chunk * 256 * SP >= vis.nv) return;              // the same for the whole workgroup
     const int tph = 256 / heads;                         // threads per head (heads <= 256)
     {
         const int hh = tid / tph, sub = tid % tph;
@@ -477,32 +495,30 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t bloc
     }
     __syncthreads();
     if (i >= vis.nv) return;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    typedef float vec __attribute__((ext_vector_type(SP)));
+    vec acc = 0.0f;
     const float* x = a.logits + bh0 * a.ld + i;
 #pragma unroll 8
     for (int hh = 0; hh < heads; ++hh) {
-        const float4 v = *reinterpret_cast<const float4*>(x + (int64_t)hh * a.ld);
+        const vec v = *reinterpret_cast<const vec*>(x + (int64_t)hh * a.ld);
         const float2 st = stat[hh];
-        acc.x += exp2_ftz(v.x - st.x) * st.y;
-        acc.y += exp2_ftz(v.y - st.x) * st.y;
-        acc.z += exp2_ftz(v.z - st.x) * st.y;
-        acc.w += exp2_ftz(v.w - st.x) * st.y;
+#pragma unroll
+        for (int e = 0; e < SP; ++e) acc[e] += exp2_ftz(v[e] - st.x) * st.y;
     }
     float* s = a.s + (int64_t)b * a.s_sb + (int64_t)r * a.s_sr;
-    const float e[4] = {acc.x, acc.y, acc.z, acc.w};
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-        if (i + u < vis.nv) s[vis.token(i + u)] += e[u];
+    for (int e = 0; e < SP; ++e)
+        if (i + e < vis.nv) s[vis.token(i + e)] += acc[e];
 }
 
 // The first merge_blocks workgroups join shares, the others add weights.
-template <int NG>
+template <int NG, int LANES, int SP>
 __global__ __launch_bounds__(256, 4) void cache_merge_kernel(CacheAttnArgs a, int64_t merge_blocks)
 {
     __shared__ f32x4_v buf[256 + 128];
     float2* two = reinterpret_cast<float2*>(buf + 256);
-    if ((int64_t)blockIdx.x < merge_blocks) merge_shares<NG>(a, blockIdx.x, buf, two);
-    else add_weights(a, (int64_t)blockIdx.x - merge_blocks, two, reinterpret_cast<float2*>(buf));
+    if ((int64_t)blockIdx.x < merge_blocks) merge_shares<NG, LANES>(a, blockIdx.x, buf, two);
+    else add_weights<SP>(a, (int64_t)blockIdx.x - merge_blocks, two, reinterpret_cast<float2*>(buf));
 }
 
 template <int KT>
@@ -518,6 +534,22 @@ void launch_rows(const CacheAttnArgs& a, hipStream_t st)
     }
 }
 
+// Few shares: eight heads a workgroup; more: one head, its shares over eight
+// groups; many: a quarter of one.
+template <int SP>
+void launch_merge(const CacheAttnArgs& a, hipStream_t st)
+{
+    const int64_t bh = (int64_t)a.B * a.Hq;
+    const int form = a.nsplit <= 8 ? 0 : a.nsplit <= 64 ? 1 : 2;
+    const int64_t merge = a.nsplit <= 1 ? 0 : form == 0 ? (bh + 7) / 8 : form == 1 ? bh : 4 * bh;
+    const int64_t add = a.s ? (int64_t)a.B * a.R * a.s_chunks : 0;
+    if (merge + add == 0) return;
+    const dim3 grid((unsigned)(merge + add));
+    if (form == 0) hipLaunchKernelGGL((cache_merge_kernel<1, 32, SP>), grid, dim3(256), 0, st, a, merge);
+    else if (form == 1) hipLaunchKernelGGL((cache_merge_kernel<8, 32, SP>), grid, dim3(256), 0, st, a, merge);
+    else hipLaunchKernelGGL((cache_merge_kernel<32, 8, SP>), grid, dim3(256), 0, st, a, merge);
+}
+
 }  // namespace
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st)
@@ -526,14 +558,8 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, int dtype, hipStream_t st)
     else if (dtype == 1) launch_rows<kRowsBf16>(a, st);
     else launch_rows<kRowsF16>(a, st);
     if (hipError_t e = hipGetLastError()) return e;
-    // few shares: eight heads a workgroup; many: one head, its shares over eight groups
-    const bool few = a.nsplit <= 8;
-    const int64_t bh = (int64_t)a.B * a.Hq;
-    const int64_t merge = a.nsplit > 1 ? (few ? (bh + 7) / 8 : bh) : 0, add = a.s ? (int64_t)a.B * a.R * a.s_chunks : 0;
-    if (merge + add == 0) return hipSuccess;
-    const dim3 grid((unsigned)(merge + add));
-    if (few) hipLaunchKernelGGL(cache_merge_kernel<1>, grid, dim3(256), 0, st, a, merge);
-    else hipLaunchKernelGGL(cache_merge_kernel<8>, grid, dim3(256), 0, st, a, merge);
+    if (a.s && a.s_per == 1) launch_merge<1>(a, st);
+    else launch_merge<4>(a, st);
     return hipGetLastError();
 }
 

@@ -649,14 +649,14 @@ struct CacheLayout {
     size_t part_o, part_ml, logits, end;
 };
 
-CacheLayout cache_layout(const hill_desc* d, const Shape& s, int ksel, bool with_s)
+CacheLayout cache_layout(const hill_desc* d, const Shape& s, int ksel, bool with_s, bool packed)
 {
     CacheLayout L{};
     int64_t seen = (int64_t)d->n_sink + d->n_recent;
     if (ksel > 0) seen = ksel;
     else if (seen > s.n) seen = s.n;
     L.head_tiles = (s.G + 15) / 16;
-    L.nsplit = cache_splits((int64_t)s.B * s.Hkv * L.head_tiles, seen);
+    L.nsplit = cache_splits((int64_t)s.B * s.Hkv * L.head_tiles, seen, packed);
     L.wgs = (int64_t)s.B * s.Hkv * L.head_tiles * L.nsplit;
     L.ld = (seen + 31) / 32 * 32;
     const size_t bh = (size_t)s.B * s.Hq;
@@ -874,7 +874,7 @@ hill_status hill_window_workspace_bytes(const hill_desc* d, int32_t n_new, size_
     HILL_TRY(check_desc(d, &s, false));
     if (n_new < 0 || n_new > s.n) return fail(HILL_ERR_INVALID_ARG, "n_new %d not in [0, n_tokens=%d]", n_new, s.n);
     if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = n_new == 0 ? cache_layout(d, s, 0, false).end : 0;
+    *bytes = n_new == 0 ? cache_layout(d, s, 0, false, false).end : 0;
     return HILL_OK;
 }
 
@@ -888,8 +888,8 @@ hill_status hill_window_attn(const hill_desc* d, const void* q, const void* k, c
     HILL_TRY(check_ptr(v, "v"));
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
-    const CacheLayout L = cache_layout(d, s, 0, false);
-    HILL_TRY(check_grid(L.wgs + (int64_t)s.B * s.Hq));
+    const CacheLayout L = cache_layout(d, s, 0, false, false);
+    HILL_TRY(check_grid(L.wgs + 4 * (int64_t)s.B * s.Hq));
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
     a.k = static_cast<const uint16_t*>(k);
@@ -1006,7 +1006,7 @@ hill_status hill_packed_workspace_bytes(const hill_desc* d, int32_t k_sel, int32
     HILL_TRY(check_desc(d, &s, false));
     if (k_sel != 0) HILL_TRY(check_ksel(s, k_sel));
     if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = cache_layout(d, s, k_sel, with_s != 0).end;
+    *bytes = cache_layout(d, s, k_sel, with_s != 0, true).end;
     return HILL_OK;
 }
 
@@ -1028,9 +1028,9 @@ hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, const voi
     }
     if (s_acc) HILL_TRY(check_ptr(s_acc, "s"));
     HILL_TRY(check_ptr(out, "out"));
-    const CacheLayout L = cache_layout(d, s, idx ? k_sel : 0, s_acc != nullptr);
-    const int s_chunks = (int)((L.ld + kScoreChunk - 1) / kScoreChunk);
-    HILL_TRY(check_grid(L.wgs + (int64_t)s.B * s.Hq + (int64_t)s.B * s.R * s_chunks));
+    const CacheLayout L = cache_layout(d, s, idx ? k_sel : 0, s_acc != nullptr, true);
+    const int s_per = score_per_thread((int64_t)s.B * s.R, L.ld), s_chunks = (int)((L.ld + 256 * s_per - 1) / (256 * s_per));
+    HILL_TRY(check_grid(L.wgs + 4 * (int64_t)s.B * s.Hq + (int64_t)s.B * s.R * s_chunks));
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
     uint8_t *kc, *vc;
@@ -1051,6 +1051,7 @@ hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, const voi
         a.s_sr = d->s_stride_r;
         a.logits = at<float>(ws, L.logits);
         a.ld = L.ld;
+        a.s_per = s_per;
         a.s_chunks = s_chunks;
     }
     HIP_TRY(launch_cache_attn(a, s.dtype, static_cast<hipStream_t>(stream)));

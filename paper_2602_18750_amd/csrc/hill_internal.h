@@ -418,15 +418,19 @@ struct CacheAttnArgs {
     int64_t s_sb, s_sr;
     float* logits;            //   [B,Hq,ld] by visible position, ld a multiple of 32
     int64_t ld;
-    int s_chunks;             //   kScoreChunk-position chunks per row
+    int s_per, s_chunks;      //   positions per thread (score_per_thread); chunks of 256 * s_per per row
 };
-constexpr int kScoreChunk = 1024;
-// Shares of `seen` visible positions: one where (sequence, KV head) pairs alone
-// give every CU a workgroup (of 256), so that nothing is left to join; else
-// about two workgroups per CU, each of at least four 32-token tiles, one per wave.
-inline int cache_splits(int64_t wgs, int64_t seen)
+// Positions per thread of the workgroups that add weights to S: four (16-byte
+// loads) where they still make a workgroup per CU, else one.
+inline int score_per_thread(int64_t rows, int64_t seen) { return rows * ((seen + 1023) / 1024) >= 256 ? 4 : 1; }
+// Shares of `seen` visible positions: about two workgroups per CU (of 256) in
+// all, each of at least four 32-token tiles, one per wave.  Where the (sequence,
+// KV head) pairs alone give every CU a workgroup, one share, and nothing to join: four waves' 16-bit
+// rows (64 KiB in flight) load a CU; packed rows (20 KiB) do not, and long ones are worth the join.
+inline int cache_splits(int64_t wgs, int64_t seen, bool packed)
 {
-    const int64_t want = wgs >= 256 ? 1 : (512 + wgs / 2) / wgs, most = (seen + 127) / 128;
+    const int64_t alone = packed && seen >= 4096 ? 512 : 256;
+    const int64_t want = wgs >= alone ? 1 : (512 + wgs / 2) / wgs, most = (seen + 127) / 128;
     const int64_t s = want < most ? want : most;
     return s < 1 ? 1 : (int)s;
 }

@@ -47,7 +47,7 @@ __device__ __forceinline__ f32x16_v mfma32(uint4 a, uint4 b, f32x16_v c)
 // Transposing LDS read: the sixteen lanes of a group point at four rows of
 // sixteen 16-bit elements, lane i at elements 4 * (i % 4) on of row i / 4, and
 // lane i receives element i of the four rows.
-__device__ __forceinline__ u32x2_v read_transposed(const uint16_t* p)
+__device__ __forceinline__ u32x2_v read_transposed(const void* p)
 {
     typedef __attribute__((address_space(3))) short4_v* lds_ptr;
     return __builtin_bit_cast(u32x2_v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p));
@@ -66,6 +66,11 @@ constexpr int kWeightTerms = DT == 1 ? 3 : 2;
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi)
 {
     return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+
+__device__ __forceinline__ uint32_t lower_halves(uint32_t lo, uint32_t hi)
+{
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 
 // Eight weights as kWeightTerms<DT> operands.
@@ -114,6 +119,23 @@ __device__ __forceinline__ uint4 decode8(uint32_t x, half2_t scale, half2_t zero
         const half2_t hi = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (y & 0x00f000f0u) | exponent), k16th, k64);
         r[s] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(lo, scale, zero));
         r[s + 1] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(hi, scale, zero));
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// The same values in the order (0, 4), (1, 5), (2, 6), (3, 7), two operations in
+// thirteen fewer: a byte that holds a code is, read as fp8 e4m3, exactly code * 2^-9 (its
+// subnormals and first binade), and one conversion makes two fp16 numbers of them.
+__device__ __forceinline__ uint4 decode8_split(uint32_t x, half2_t scale, half2_t zero)
+{
+    const uint32_t y[2] = {x & 0x0f0f0f0fu, (x >> 4) & 0x0f0f0f0fu};
+    uint32_t r[4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const half2_t c0 = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y[s], 512.0f, false));
+        const half2_t c1 = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(y[s], 512.0f, true));
+        r[2 * s] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c0, scale, zero));
+        r[2 * s + 1] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c1, scale, zero));
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }

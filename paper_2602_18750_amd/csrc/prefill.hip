@@ -24,12 +24,14 @@ namespace hill {
 namespace {
 
 constexpr int kKeys = 64;                       // tokens per tile
-constexpr int kTileHalfs = kKeys * kHeadDim;    // 16-bit elements of a K or V tile
+// A tile in LDS: blocks of four rows, which one direct load of a wave fills, each
+// 16 bytes further than its 1 KiB; row r of a block keeps its 16-byte piece c at c ^
+// 4r.  The rows of one access then lie in different banks (sixteen rows in a column of K;
+// four rows by 64 bytes of V), and all of a lane's addresses are one of four and a constant.
+constexpr int kBlockBytes = 4 * kHeadDim * 2 + 16;
+constexpr int kTileBytes = kKeys / 4 * kBlockBytes;
 constexpr float kSlack = 8.0f;
-
-// Rows of a tile are 16 pieces of 16 bytes; row j keeps piece c at c ^ swizzle(j), so that the rows that one LDS
-// access touches (16 in a column of K, four by four of V) lie in different banks.
-__device__ __forceinline__ int swizzle(int j) { return ((j & 3) << 2) | ((j >> 2) & 3); }
+constexpr int kMfma = 0x008, kDsRead = 0x100;   // instruction kinds for scheduling groups
 
 __device__ __forceinline__ float max_x32(float v)
 {
@@ -45,7 +47,7 @@ __device__ __forceinline__ uint32_t round_pair(float x, float y)
 }
 
 // 16 bytes per lane from global memory into LDS, lane after lane from `to` on.
-__device__ __forceinline__ void load_lds16(const uint16_t* from, uint16_t* to)
+__device__ __forceinline__ void load_lds16(const uint16_t* from, char* to)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
 {
     // four arrays of their own, each step's named at compile time: the compiler then knows that the direct loads into one
     // pair do not write what is read from the other, and does not wait for them before the first read
-    __shared__ __attribute__((aligned(16))) uint16_t k0[kTileHalfs], v0[kTileHalfs], k1[kTileHalfs], v1[kTileHalfs];
+    __shared__ __attribute__((aligned(16))) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
     const int tid = threadIdx.x, lane = tid & 63, c32 = lane & 31, hf = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (sequence, KV head) fastest, so that its blocks meet its K and V in one L2; the last tokens, whose windows
@@ -92,15 +94,15 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
         const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh;
         auto tile_begin = [&](int t) { return t < st ? t * kKeys : ws + (t - st) * kKeys; };
         auto tile_end = [&](int t) { return t < st ? min(ns, (t + 1) * kKeys) : min(pb + 1, ws + (t - st + 1) * kKeys); };
-        auto load = [&](int t, uint16_t* kl, uint16_t* vl) {   // rows past the tile's end repeat its last one (they weigh 0)
+        auto load = [&](int t, char* kl, char* vl) {   // rows past the tile's end repeat its last one (they weigh 0)
             const int j0 = tile_begin(t), jl = tile_end(t) - 1;
+            const int piece = (lane & 15) ^ (4 * (lane >> 4));
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int jr = 16 * u + 4 * w + (lane >> 4);
-                const int piece = (lane & 15) ^ swizzle(jr);
-                const uint32_t j = (uint32_t)min(j0 + jr, jl);
-                load_lds16(kb + (uint64_t)j * (uint32_t)a.k_sn + piece * 8, kl + (16 * u + 4 * w) * kHeadDim);
-                load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + (16 * u + 4 * w) * kHeadDim);
+                const int block = 4 * u + w;
+                const uint32_t j = (uint32_t)min(j0 + 4 * block + (lane >> 4), jl);
+                load_lds16(kb + (uint64_t)j * (uint32_t)a.k_sn + piece * 8, kl + block * kBlockBytes);
+                load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + block * kBlockBytes);
             }
         };
         load(0, k0, v0);
@@ -114,9 +116,15 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
             qf[i] = make_uint4(qf[i].x ^ flip, qf[i].y ^ flip, qf[i].z ^ flip, qf[i].w ^ flip);
         }
 
-        // this lane's LDS offsets (elements): K piece (2i + hf) of row c32 (+ 32), V rows 4 hf + (c16 / 4) on
-        const int c16 = lane & 15, vrow = 4 * hf + (c16 >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((c16 & 3) >> 1);
-        auto step = [&](int t, const uint16_t* kl, const uint16_t* vl, uint16_t* kn, uint16_t* vn) {
+        // this lane's LDS offsets: K row c32, pieces 4x + hf on; V row 4 hf + c16 / 4, pieces 4x + its half of 32 columns
+        const int c16 = lane & 15, vpiece = 2 * ((lane >> 4) & 1) + ((c16 & 3) >> 1);
+        int ka[4], va[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            ka[x] = (c32 >> 2) * kBlockBytes + (c32 & 3) * 256 + ((4 * x + hf) ^ (4 * (c32 & 3))) * 16;
+            va[x] = hf * kBlockBytes + (c16 >> 2) * 256 + ((4 * x + vpiece) ^ (4 * (c16 >> 2))) * 16 + 8 * (c16 & 1);
+        }
+        auto step = [&](int t, const char* kl, const char* vl, char* kn, char* vn) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();       // tile t is there, and every wave has left tile t - 1
             if (t + 1 < nt) load(t + 1, kn, vn);
@@ -126,15 +134,23 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
             f32x16_v x[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
+                uint4 kf[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    kf[i] = *reinterpret_cast<const uint4*>(kl + ka[i >> 1] + 32 * (i & 1) + 8 * s * kBlockBytes);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[s][e] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int jr = 32 * s + c32;
-                    const uint4 kf = *reinterpret_cast<const uint4*>(kl + jr * kHeadDim + (((2 * i + hf) ^ swizzle(jr)) * 8));
-                    x[s] = mfma32<DT>(kf, qf[i], x[s]);
-                }
+                for (int i = 0; i < 8; ++i) x[s] = mfma32<DT>(kf[i], qf[i], x[s]);
             }
+            // LDS reads run six products ahead
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
+#pragma unroll
+            for (int i = 0; i < 10; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kMfma, 6, 0);
             // every row of the wave sees the whole tile, or masks
             const bool whole = j1 - j0 == kKeys && j1 - 1 <= pw0 && (j1 <= a.sink || j0 > pw1 - a.window);
             float mx = -INFINITY;
@@ -182,12 +198,10 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
                 }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {                       // 16 tokens each
-                const int ja = 16 * q + vrow, jb = ja + 8;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const int piece = 4 * d + vpiece;
-                    const u32x2_v lo = read_transposed(vl + ja * kHeadDim + ((piece ^ swizzle(ja)) * 8) + 4 * (c16 & 1));
-                    const u32x2_v hi = read_transposed(vl + jb * kHeadDim + ((piece ^ swizzle(jb)) * 8) + 4 * (c16 & 1));
+                    const u32x2_v lo = read_transposed(vl + va[d] + 4 * q * kBlockBytes);
+                    const u32x2_v hi = read_transposed(vl + va[d] + (4 * q + 2) * kBlockBytes);
                     o[d] = mfma32<DT>(make_uint4(lo.x, lo.y, hi.x, hi.y), pf[q], o[d]);
                 }
             }
