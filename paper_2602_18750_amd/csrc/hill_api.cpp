@@ -927,7 +927,8 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
     HILL_TRY(check_ws(ws, ws_bytes, 0));
-    const int64_t blocks = ((int64_t)p->n_new * s.G + kPrefillRows - 1) / kPrefillRows;
+    const int per_wg = prefill_rows((int64_t)s.B * s.Hkv, (int64_t)p->n_new * s.G);
+    const int64_t blocks = ((int64_t)p->n_new * s.G + per_wg - 1) / per_wg;
     HILL_TRY(check_grid((int64_t)s.B * s.Hkv * blocks));
     PrefillArgs a{};
     a.q = static_cast<const uint16_t*>(q);
@@ -955,6 +956,7 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     a.t = p->n_new;
     a.sink = d->n_sink < s.n ? d->n_sink : s.n;           // more than the cache holds is all of it (no overflow
     a.window = d->n_recent < s.n ? d->n_recent : s.n;     // on the device)
+    a.rows_per_wg = per_wg;
     a.blocks = (int)blocks;
     a.s2 = s.scale * 1.4426950408889634f;
     HIP_TRY(launch_prefill(a, s.dtype, static_cast<hipStream_t>(stream)));

@@ -463,10 +463,10 @@ struct PrefillArgs {
     int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
     const int32_t* lens;
     int B, Hq, Hkv, G, n, t, sink, window;
-    int blocks;               // row blocks per (b, KV head)
+    int rows_per_wg, blocks;  // (token, head) rows per workgroup; such blocks per (b, KV head)
     float s2;
 };
-constexpr int kPrefillRows = 128;   // (token, head) rows per workgroup
+inline int prefill_rows(int64_t bh, int64_t rows) { return bh * ((rows + 255) / 256) >= 256 ? 256 : 128; }
 hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st);
 
 // Kept rows moved to the front (evict.hip).

@@ -53,9 +53,10 @@ __device__ __forceinline__ void load_lds16(const uint16_t* from, char* to)
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-template <int DT>
-__global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
+template <int DT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
 {
+    constexpr int kRows = 32 * NW;
     // four arrays of their own, each step's named at compile time: the compiler then knows that the direct loads into one
     // pair do not write what is read from the other, and does not wait for them before the first read
     __shared__ __attribute__((aligned(16))) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
@@ -68,11 +69,11 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
     const int len = seq_len(a.lens, b, a.n);
     const int first = len - a.t;                            // position of the chunk's first token (may be < 0)
     const int rows = a.t * a.G;
-    const int r0 = blk * kPrefillRows;
+    const int r0 = blk * kRows;
     const int row = min(r0 + 32 * w + c32, rows - 1);       // this lane's row
     const int tq = row / a.G, hq = g * a.G + row % a.G;
     const int p = first + tq;
-    const int pa = max(first + r0 / a.G, 0), pb = first + min(r0 + kPrefillRows - 1, rows - 1) / a.G;
+    const int pa = max(first + r0 / a.G, 0), pb = first + min(r0 + kRows - 1, rows - 1) / a.G;
 
     uint16_t* out = a.out + (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)tq * a.o_st;
     const bool live = r0 + 32 * w + c32 < rows;
@@ -98,13 +99,14 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
             const int j0 = tile_begin(t), jl = tile_end(t) - 1;
             const int piece = (lane & 15) ^ (4 * (lane >> 4));
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int block = 4 * u + w;
+            for (int u = 0; u < kKeys / 4 / NW; ++u) {
+                const int block = NW * u + w;
                 const uint32_t j = (uint32_t)min(j0 + 4 * block + (lane >> 4), jl);
                 load_lds16(kb + (uint64_t)j * (uint32_t)a.k_sn + piece * 8, kl + block * kBlockBytes);
                 load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + block * kBlockBytes);
             }
         };
+        if (NW == 8 && w < 4) __builtin_amdgcn_s_setprio(1);
         load(0, k0, v0);
         uint4 qf[8];
         const float s2 = fabsf(a.s2);                   // a negative scale goes into the query's signs
@@ -133,16 +135,16 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
             if (j0 > pw1 || (j0 >= a.sink && j1 - 1 <= pw0 - a.window)) return;
             f32x16_v x[2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                uint4 kf[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    kf[i] = *reinterpret_cast<const uint4*>(kl + ka[i >> 1] + 32 * (i & 1) + 8 * s * kBlockBytes);
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[s][e] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[s] = mfma32<DT>(kf[i], qf[i], x[s]);
-            }
+            for (int i = 0; i < 8; ++i)      // the two halves in turn: a product waits for the one before it on the same sums
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const uint4 kf = *reinterpret_cast<const uint4*>(kl + ka[i >> 1] + 32 * (i & 1) + 8 * s * kBlockBytes);
+                    x[s] = mfma32<DT>(kf, qf[i], x[s]);
+                }
             // LDS reads run six products ahead
             __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
 #pragma unroll
@@ -229,8 +231,13 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(PrefillArgs a)
 hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st)
 {
     const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.blocks));
-    if (dtype == 1) hipLaunchKernelGGL(prefill_kernel<1>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(prefill_kernel<0>, grid, dim3(256), 0, st, a);
+    if (a.rows_per_wg == 256) {
+        if (dtype == 1) hipLaunchKernelGGL((prefill_kernel<1, 8>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((prefill_kernel<0, 8>), grid, dim3(512), 0, st, a);
+    } else {
+        if (dtype == 1) hipLaunchKernelGGL((prefill_kernel<1, 4>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((prefill_kernel<0, 4>), grid, dim3(256), 0, st, a);
+    }
     return hipGetLastError();
 }
 
