@@ -387,66 +387,11 @@ __global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_ker
     }
 }
 
-// Joins shares: LANES lanes of four dimensions each (32: a whole head) in NG
-// groups make a head, or a quarter of one; group i takes shares i, i + NG, ...
-// with up to eight loads in flight.  Empty shares have l = 0, and a head without any l gives 0.
 template <int NG, int LANES>
 __device__ __forceinline__ void merge_shares(const CacheAttnArgs& a, int64_t block, f32x4_v* osum, float2* mlsum)
 {
-    constexpr int kParts = 32 / LANES, kPerWg = 256 / (NG * LANES);   // parts of a head; (head, part) pairs per workgroup
-    const int tid = threadIdx.x, grp = tid / LANES % NG;
-    const int64_t pairs = (int64_t)a.B * a.Hq * kParts, mine = block * kPerWg + tid / (NG * LANES);
-    const int64_t bp = mine < pairs ? mine : pairs - 1;     // past the last: it again, not stored
-    const int64_t bh = bp / kParts;
-    const int d = 4 * (tid % LANES + LANES * (int)(bp % kParts));
-    const float2* ml = a.part_ml + bh * a.nsplit;
-    const float* po = a.part_o + bh * a.nsplit * kHeadDim + d;
-    float m = -INFINITY, l = 0.0f;
-    f32x4_v o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s0 = grp; s0 < a.nsplit; s0 += 8 * NG) {
-        float2 v[8];
-        f32x4_v x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {                       // past the last share: it again, with weight 0
-            const int s = min(s0 + i * NG, a.nsplit - 1);
-            v[i] = ml[s];
-            x[i] = *reinterpret_cast<const f32x4_v*>(po + (int64_t)s * kHeadDim);
-            if (s0 + i * NG >= a.nsplit) v[i].y = 0.0f;
-        }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].y > 0.0f ? v[i].x : -INFINITY);
-        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
-        o *= al;
-        l *= al;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = v[i].y > 0.0f ? exp2_ftz(v[i].x - top) : 0.0f;
-            o += f * x[i];
-            l += f * v[i].y;
-        }
-        m = top;
-    }
-    if constexpr (NG > 1) {
-        osum[tid] = o;
-        mlsum[tid] = make_float2(m, l);
-        __syncthreads();
-        if (grp != 0) return;
-        float top = m;
-#pragma unroll 8
-        for (int i = 1; i < NG; ++i) top = fmaxf(top, mlsum[tid + LANES * i].x);
-        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
-        o *= al;
-        l *= al;
-#pragma unroll 8
-        for (int i = 1; i < NG; ++i) {
-            const float2 v = mlsum[tid + LANES * i];
-            const float f = v.y > 0.0f ? exp2_ftz(v.x - top) : 0.0f;
-            o += f * osum[tid + LANES * i];
-            l += f * v.y;
-        }
-    }
-    if (mine < pairs) *reinterpret_cast<f32x4_v*>(a.out + bh * kHeadDim + d) = l > 0.0f ? o * (1.0f / l) : o * 0.0f;
+    const Joined j = join_shares<NG, LANES>(a.part_o, a.part_ml, a.nsplit, (int64_t)a.B * a.Hq, block, osum, mlsum);
+    if (j.row >= 0) *reinterpret_cast<f32x4_v*>(a.out + j.row * kHeadDim + j.d) = j.o;
 }
 
 // S[b, r, j(i)] += the weights of the row's heads, 256 * SP positions per

@@ -698,6 +698,30 @@ CacheAttnArgs cache_args(const hill_desc* d, const Shape& s, const CacheLayout& 
     return a;
 }
 
+// Blocks, shares and workspace of a prefill: partial outputs and (max, sum) per row and share.
+struct PrefillLayout {
+    int rows_per_wg, nsplit;
+    int64_t blocks, wgs;
+    size_t part_ml, end;
+};
+
+PrefillLayout prefill_layout(const hill_desc* d, const Shape& s, int n_new)
+{
+    PrefillLayout L{};
+    const int64_t bh = (int64_t)s.B * s.Hkv, rows = (int64_t)n_new * s.G;
+    L.rows_per_wg = prefill_rows(bh, rows);
+    L.blocks = (rows + L.rows_per_wg - 1) / L.rows_per_wg;
+    int64_t seen = (int64_t)d->n_sink + d->n_recent + L.rows_per_wg / s.G;   // tokens of a block's walk at most
+    if (seen > s.n) seen = s.n;
+    L.nsplit = prefill_splits(bh * L.blocks, seen);
+    L.wgs = bh * L.blocks * L.nsplit;
+    if (L.nsplit > 1) {
+        L.part_ml = align256((size_t)bh * rows * L.nsplit * kHeadDim * sizeof(float));
+        L.end = L.part_ml + align256((size_t)bh * rows * L.nsplit * sizeof(float2));
+    }
+    return L;
+}
+
 void set_packed(const hill_packed* p, uint8_t** kc, uint8_t** vc, uint32_t** kp, uint32_t** vp)
 {
     *kc = static_cast<uint8_t*>(p->k_codes);
@@ -874,7 +898,7 @@ hill_status hill_window_workspace_bytes(const hill_desc* d, int32_t n_new, size_
     HILL_TRY(check_desc(d, &s, false));
     if (n_new < 0 || n_new > s.n) return fail(HILL_ERR_INVALID_ARG, "n_new %d not in [0, n_tokens=%d]", n_new, s.n);
     if (!bytes) return fail(HILL_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = n_new == 0 ? cache_layout(d, s, 0, false, false).end : 0;
+    *bytes = n_new == 0 ? cache_layout(d, s, 0, false, false).end : prefill_layout(d, s, n_new).end;
     return HILL_OK;
 }
 
@@ -926,10 +950,9 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     HILL_TRY(check_ptr(v, "v"));
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
-    HILL_TRY(check_ws(ws, ws_bytes, 0));
-    const int per_wg = prefill_rows((int64_t)s.B * s.Hkv, (int64_t)p->n_new * s.G);
-    const int64_t blocks = ((int64_t)p->n_new * s.G + per_wg - 1) / per_wg;
-    HILL_TRY(check_grid((int64_t)s.B * s.Hkv * blocks));
+    const PrefillLayout L = prefill_layout(d, s, p->n_new);
+    HILL_TRY(check_grid(L.wgs > (int64_t)s.B * s.Hq * p->n_new ? L.wgs : (int64_t)s.B * s.Hq * p->n_new));
+    HILL_TRY(check_ws(ws, ws_bytes, L.end));
     PrefillArgs a{};
     a.q = static_cast<const uint16_t*>(q);
     a.k = static_cast<const uint16_t*>(k);
@@ -956,8 +979,13 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     a.t = p->n_new;
     a.sink = d->n_sink < s.n ? d->n_sink : s.n;           // more than the cache holds is all of it (no overflow
     a.window = d->n_recent < s.n ? d->n_recent : s.n;     // on the device)
-    a.rows_per_wg = per_wg;
-    a.blocks = (int)blocks;
+    a.rows_per_wg = L.rows_per_wg;
+    a.blocks = (int)L.blocks;
+    a.nsplit = L.nsplit;
+    if (L.nsplit > 1) {
+        a.part_o = at<float>(ws, 0);
+        a.part_ml = at<float2>(ws, L.part_ml);
+    }
     a.s2 = s.scale * 1.4426950408889634f;
     HIP_TRY(launch_prefill(a, s.dtype, static_cast<hipStream_t>(stream)));
     return HILL_OK;

@@ -464,9 +464,23 @@ struct PrefillArgs {
     const int32_t* lens;
     int B, Hq, Hkv, G, n, t, sink, window;
     int rows_per_wg, blocks;  // (token, head) rows per workgroup; such blocks per (b, KV head)
+    int nsplit;               // shares of a block's tokens
+    float* part_o;            // [B,Hkv,t*G,nsplit,D] (nsplit > 1)
+    float2* part_ml;          // [B,Hkv,t*G,nsplit]
     float s2;
 };
+// Rows per workgroup: 256 (eight waves) where that gives every CU one (of 256), since a workgroup's rows share the
+// keys and values it reads (16K x 16K tokens, window 4096: 986 -> 955 us); else 128.
 inline int prefill_rows(int64_t bh, int64_t rows) { return bh * ((rows + 255) / 256) >= 256 ? 256 : 128; }
+// Shares: where 128-row blocks leave a third of the two workgroups per CU without work, as many as fill them, of at
+// least two 64-token tiles each.  One sequence, GQA 32/8, window 4096, one share -> several (us): 640 new tokens (160
+// blocks) 88.8 -> 69.3; on the other side 800 (200 blocks) 87.0 and 88.7, 1024 (256) 92.9 and 95.2.
+inline int prefill_splits(int64_t wgs, int64_t seen)
+{
+    if (wgs > 170) return 1;
+    const int64_t want = 512 / wgs, most = (seen + 127) / 128;
+    return (int)(want < most ? want : most < 1 ? 1 : most);
+}
 hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st);
 
 // Kept rows moved to the front (evict.hip).

@@ -148,6 +148,81 @@ __device__ __forceinline__ void group_params(uint32_t par, half2_t& scale, half2
     zero = half2_t{p[1], p[1]};
 }
 
+// Four dimensions (from d on) of a row's output; row < 0: nothing to write.
+struct Joined {
+    int64_t row;
+    int d;
+    f32x4_v o;
+};
+
+// Joins the shares of attention rows (unnormalised outputs part_o [rows, nsplit,
+// 128], (max, sum) part_ml [rows, nsplit]) in a workgroup of 256 threads:
+// LANES lanes of four dimensions each (32: a whole row) in NG groups make a row, or
+// a quarter of one; group i takes shares i, i + NG, ... with up to eight loads in
+// flight.  Empty shares have sum 0, and a row without any gives 0.
+template <int NG, int LANES>
+__device__ __forceinline__ Joined join_shares(const float* part_o, const float2* part_ml, int nsplit, int64_t rows, int64_t block,
+                                              f32x4_v* osum, float2* mlsum)
+{
+    constexpr int kParts = 32 / LANES, kPerWg = 256 / (NG * LANES);   // parts of a row; (row, part) pairs per workgroup
+    const int tid = threadIdx.x, grp = tid / LANES % NG;
+    const int64_t pairs = rows * kParts, mine = block * kPerWg + tid / (NG * LANES);
+    const int64_t rp = mine < pairs ? mine : pairs - 1;               // past the last: it again
+    Joined r;
+    r.d = 4 * (tid % LANES + LANES * (int)(rp % kParts));
+    r.row = rp / kParts;
+    const float2* ml = part_ml + r.row * nsplit;
+    const float* po = part_o + r.row * nsplit * kHeadDim + r.d;
+    if (mine >= pairs) r.row = -1;
+    float m = -INFINITY, l = 0.0f;
+    f32x4_v o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = grp; s0 < nsplit; s0 += 8 * NG) {
+        float2 v[8];
+        f32x4_v x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                                 // past the last share: it again, with weight 0
+            const int s = min(s0 + i * NG, nsplit - 1);
+            v[i] = ml[s];
+            x[i] = *reinterpret_cast<const f32x4_v*>(po + (int64_t)s * kHeadDim);
+            if (s0 + i * NG >= nsplit) v[i].y = 0.0f;
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].y > 0.0f ? v[i].x : -INFINITY);
+        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
+        o *= al;
+        l *= al;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float f = v[i].y > 0.0f ? exp2_ftz(v[i].x - top) : 0.0f;
+            o += f * x[i];
+            l += f * v[i].y;
+        }
+        m = top;
+    }
+    if constexpr (NG > 1) {
+        osum[tid] = o;
+        mlsum[tid] = make_float2(m, l);
+        __syncthreads();
+        if (grp != 0) r.row = -1;
+        float top = m;
+#pragma unroll 8
+        for (int i = 1; i < NG; ++i) top = fmaxf(top, mlsum[(tid + LANES * i) & 255].x);
+        const float al = l > 0.0f ? exp2_ftz(m - top) : 0.0f;
+        o *= al;
+        l *= al;
+#pragma unroll 8
+        for (int i = 1; i < NG; ++i) {
+            const float2 v = mlsum[(tid + LANES * i) & 255];          // (groups other than 0 add to no avail)
+            const float f = v.y > 0.0f ? exp2_ftz(v.x - top) : 0.0f;
+            o += f * osum[(tid + LANES * i) & 255];
+            l += f * v.y;
+        }
+    }
+    r.o = l > 0.0f ? o * (1.0f / l) : o * 0.0f;
+    return r;
+}
+
 // Which tokens a query sees: the first ns and, gap tokens further, the last
 // nw of a sequence of `len`.  Position i of the ns + nw visible ones is token
 // i + (i < ns ? 0 : gap).

@@ -64,7 +64,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (sequence, KV head) fastest, so that its blocks meet its K and V in one L2; the last tokens, whose windows
     // are full, first
-    const int bh = blockIdx.x % (a.B * a.Hkv), blk = a.blocks - 1 - (int)(blockIdx.x / (a.B * a.Hkv));
+    const int split = blockIdx.x % a.nsplit, unit = blockIdx.x / a.nsplit;
+    const int bh = unit % (a.B * a.Hkv), blk = a.blocks - 1 - unit / (a.B * a.Hkv);
     const int b = bh / a.Hkv, g = bh % a.Hkv;
     const int len = seq_len(a.lens, b, a.n);
     const int first = len - a.t;                            // position of the chunk's first token (may be < 0)
@@ -75,7 +76,6 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
     const int p = first + tq;
     const int pa = max(first + r0 / a.G, 0), pb = first + min(r0 + kRows - 1, rows - 1) / a.G;
 
-    uint16_t* out = a.out + (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)tq * a.o_st;
     const bool live = r0 + 32 * w + c32 < rows;
 
     f32x16_v o[4];
@@ -89,7 +89,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
         // tokens [0, ns) and [ws, pb]
         const int ws = max(pa - a.window + 1, 0);
         const int ns = min(a.sink, ws);
-        const int st = (ns + kKeys - 1) / kKeys, nt = st + (pb + 1 - ws + kKeys - 1) / kKeys;
+        const int st = (ns + kKeys - 1) / kKeys, all = st + (pb + 1 - ws + kKeys - 1) / kKeys;
+        const int per = (all + a.nsplit - 1) / a.nsplit, tb = split * per, nt = min(all, tb + per);   // this share's tiles
         const int pw0 = __builtin_amdgcn_readfirstlane(p), pw1 = __builtin_amdgcn_readlane(p, 31);   // this wave's positions
         const uint16_t* kb = a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh;
         const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
             }
         };
         if (NW == 8 && w < 4) __builtin_amdgcn_s_setprio(1);
-        load(0, k0, v0);
+        if (tb < nt) load(tb, k0, v0);
         uint4 qf[8];
         const float s2 = fabsf(a.s2);                   // a negative scale goes into the query's signs
         const uint32_t flip = a.s2 < 0.0f ? 0x80008000u : 0u;
@@ -208,14 +209,27 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
                 }
             }
         };
-        for (int t = 0; t < nt; t += 2) {
+        for (int t = tb; t < nt; t += 2) {
             step(t, k0, v0, k1, v1);
             if (t + 1 < nt) step(t + 1, k1, v1, k0, v0);
         }
     }
     l += __shfl_xor(l, 32, 64);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;               // nothing visible: 0
     if (!live) return;
+    if (a.nsplit > 1) {                                         // a share: unnormalised, by row, joined afterwards
+        const int64_t i = ((int64_t)bh * rows + row) * a.nsplit + split;
+        if (hf == 0) a.part_ml[i] = make_float2(m, l);
+        float* to = a.part_o + i * kHeadDim;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<f32x4_v*>(to + 32 * d + 8 * e + 4 * hf) =
+                    f32x4_v{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+        return;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;               // nothing visible: 0
+    uint16_t* out = a.out + (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)tq * a.o_st;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -226,18 +240,39 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
         }
 }
 
+// The shares of row (bh, token, head of the group) joined and written in the cache's type.
+template <int DT, int NG>
+__global__ __launch_bounds__(256, 4) void prefill_merge_kernel(PrefillArgs a)
+{
+    __shared__ f32x4_v osum[256];
+    __shared__ float2 mlsum[256];
+    const int64_t per = (int64_t)a.t * a.G;
+    const Joined j = join_shares<NG, 32>(a.part_o, a.part_ml, a.nsplit, a.B * a.Hkv * per, blockIdx.x, osum, mlsum);
+    if (j.row < 0) return;
+    const int bh = (int)(j.row / per), row = (int)(j.row % per);
+    uint16_t* out = a.out + (int64_t)(bh / a.Hkv) * a.o_sb + (int64_t)(bh % a.Hkv * a.G + row % a.G) * a.o_sh +
+                    (int64_t)(row / a.G) * a.o_st + j.d;
+    *reinterpret_cast<uint2*>(out) = make_uint2(round_pair<DT>(j.o[0], j.o[1]), round_pair<DT>(j.o[2], j.o[3]));
+}
+
+template <int DT>
+void launch_type(const PrefillArgs& a, hipStream_t st)
+{
+    const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.blocks * a.nsplit));
+    if (a.rows_per_wg == 256) hipLaunchKernelGGL((prefill_kernel<DT, 8>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((prefill_kernel<DT, 4>), grid, dim3(256), 0, st, a);
+    if (a.nsplit == 1) return;
+    const int64_t rows = (int64_t)a.B * a.Hq * a.t;
+    if (a.nsplit <= 8) hipLaunchKernelGGL((prefill_merge_kernel<DT, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((prefill_merge_kernel<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
+}
+
 }  // namespace
 
 hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st)
 {
-    const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * a.blocks));
-    if (a.rows_per_wg == 256) {
-        if (dtype == 1) hipLaunchKernelGGL((prefill_kernel<1, 8>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((prefill_kernel<0, 8>), grid, dim3(512), 0, st, a);
-    } else {
-        if (dtype == 1) hipLaunchKernelGGL((prefill_kernel<1, 4>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((prefill_kernel<0, 4>), grid, dim3(256), 0, st, a);
-    }
+    if (dtype == 1) launch_type<1>(a, st);
+    else launch_type<0>(a, st);
     return hipGetLastError();
 }
 

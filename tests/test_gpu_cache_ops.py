@@ -187,6 +187,41 @@ def test_window_prefill(case, dtype):
     check_prefill(out, q, k, v, lens or [n] * B, sink, window)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("B,Hq,Hkv,n,T,sink,window", [
+    (33, 16, 8, 500, 150, 5, 170),       # eight-wave workgroups, two blocks of 256 rows
+    (20, 8, 8, 400, 130, 40, 100),       # four-wave workgroups, one share
+    (2, 8, 2, 3000, 5, 9, 2500),         # few rows: many shares
+    (1, 12, 4, 2100, 100, 0, 2100),
+])
+def test_window_prefill_block_forms(B, Hq, Hkv, n, T, sink, window, dtype):
+    """Every form of a block and its shares, ragged lengths (some below the chunk) among them."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    q = torch.randn((B, T, Hq, D), generator=g, device=DEV).to(dtype).transpose(1, 2)
+    k, v = (torch.randn((B, Hkv, n, D), generator=g, device=DEV).to(dtype) for _ in range(2))
+    lens = torch.randint(1, n + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+    lens[0] = n
+    if B > 2:
+        lens[1], lens[2] = T // 2, 0
+    out = H().hill_window_prefill(q, k, v, window=window, n_sink=sink, lens=lens)
+    assert out.stride() == q.stride()
+    j = torch.arange(n, device=DEV)
+    p = lens.view(B, 1, 1) - T + torch.arange(T, device=DEV).view(1, T, 1)
+    seen = ((j <= p) & ((j < sink) | (p - j < window))).view(B, 1, 1, T, n)
+    x = torch.matmul(q.double().reshape(B, Hkv, Hq // Hkv * T, D), k.double().transpose(2, 3).contiguous()) * D ** -0.5
+    x = x.view(B, Hkv, Hq // Hkv, T, n).masked_fill(~seen, -1e300)
+    e = torch.where(seen, torch.exp(x - x.amax(-1, keepdim=True)), torch.zeros_like(x))
+    w = e / e.sum(-1, keepdim=True).clamp_min(1e-300)
+    want, spread = (torch.matmul(w.view(B, Hkv, -1, n), y.double()).view(B, Hq, T, D) for y in (v, v.abs()))
+    size = torch.matmul(q.double().abs().reshape(B, Hkv, -1, D), k.double().abs().transpose(2, 3).contiguous()).amax() * D ** -0.5
+    u = HALF[dtype]
+    # as check_prefill's, the largest products for every row
+    tol = (2 * (size * (D * R.F32 + 4 * R.F32 * 1.4427) + 8 * R.F32) + 2 * (n / 32 + 64) * R.F32 + u) * spread
+    tol = tol + u * (1 + u) * want.abs() + 2.0 ** -25 + (n * 2.0 ** -25 * v.abs().max().double() if dtype == torch.float16 else 0)
+    assert ((out.double() - want).abs() <= tol).all(), ((out.double() - want).abs() - tol).max()
+    assert (out.double()[~seen.any(-1).expand(B, Hkv, Hq // Hkv, T).reshape(B, Hq, T)] == 0).all()
+
+
 @pytest.mark.parametrize("scale", [0.0, 0.4, -0.3])
 def test_window_prefill_strides_scales_and_unseen_rows(scale):
     """Token-major q, out and cache; rows that no query sees full of NaN; what lies between out's rows is left."""
