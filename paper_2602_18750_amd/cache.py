@@ -304,6 +304,8 @@ def hill_evict(s, k_keep, *, k=None, v=None, cache: Optional[PackedCache] = None
     s_st = _rows("s", s, 3, torch.float32)
     B, R, cap = s.shape
     n = _tokens(n_tokens, cap, "s")
+    if not 1 <= k_keep <= n:
+        raise ValueError("k_keep %d not in [1, n_tokens=%d]" % (k_keep, n))
     k_st = v_st = None
     Hkv, dtype = n_kv_heads, torch.float16
     if k is not None:

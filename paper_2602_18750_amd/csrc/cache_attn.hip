@@ -207,7 +207,7 @@ __device__ __forceinline__ float bf16_query_to_half(uint4 (&qf)[4])
     int e = 0;
     if (m > 0.0f && m < INFINITY) {
         frexpf(m, &e);
-        e -= 15;
+        e = max(e - 15, -100);   // 2^e times the softmax scale stays a normal number
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

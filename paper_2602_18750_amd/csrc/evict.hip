@@ -20,9 +20,9 @@ namespace {
 
 constexpr int kLoads = kEvictChunk / 16;   // 16-bit rows per lane group (16 lanes a row)
 
-// A wait lasts a few microseconds; the limit (about a second) ends it where two
-// calls share one workspace at a time, against the contract.
-constexpr int kMaxSpins = 1 << 20;
+// A wait lasts a few microseconds; the limit (tens of milliseconds) ends it where
+// two calls share one workspace at a time, against the contract.
+constexpr int kMaxSpins = 1 << 16;
 
 // Stores wait for the flag seen before them, loads for the flag set after them.
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
