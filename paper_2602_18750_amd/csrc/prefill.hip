@@ -31,7 +31,6 @@ constexpr int kKeys = 64;                       // tokens per tile
 constexpr int kBlockBytes = 4 * kHeadDim * 2 + 16;
 constexpr int kTileBytes = kKeys / 4 * kBlockBytes;
 constexpr float kSlack = 8.0f;
-constexpr int kMfma = 0x008, kDsRead = 0x100;   // instruction kinds for scheduling groups
 
 __device__ __forceinline__ float max_x32(float v)
 {
@@ -96,19 +95,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
         const uint16_t* vb = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh;
         auto tile_begin = [&](int t) { return t < st ? t * kKeys : ws + (t - st) * kKeys; };
         auto tile_end = [&](int t) { return t < st ? min(ns, (t + 1) * kKeys) : min(pb + 1, ws + (t - st + 1) * kKeys); };
-        auto load = [&](int t, char* kl, char* vl) {   // rows past the tile's end repeat its last one (they weigh 0)
-            const int j0 = tile_begin(t), jl = tile_end(t) - 1;
-            const int piece = (lane & 15) ^ (4 * (lane >> 4));
+        const int piece = (lane & 15) ^ (4 * (lane >> 4));
+        auto load = [&](int t, const uint16_t* base, int64_t sn, char* to) {   // rows past the tile's end repeat its last
+            const int j0 = tile_begin(t), jl = tile_end(t) - 1;                // one (they weigh 0)
 #pragma unroll
             for (int u = 0; u < kKeys / 4 / NW; ++u) {
                 const int block = NW * u + w;
                 const uint32_t j = (uint32_t)min(j0 + 4 * block + (lane >> 4), jl);
-                load_lds16(kb + (uint64_t)j * (uint32_t)a.k_sn + piece * 8, kl + block * kBlockBytes);
-                load_lds16(vb + (uint64_t)j * (uint32_t)a.v_sn + piece * 8, vl + block * kBlockBytes);
+                load_lds16(base + (uint64_t)j * (uint32_t)sn + piece * 8, to + block * kBlockBytes);
             }
         };
-        if (NW == 8 && w < 4) __builtin_amdgcn_s_setprio(1);
-        if (tb < nt) load(tb, k0, v0);
+        if (tb < nt) {
+            load(tb, kb, a.k_sn, k0);
+            load(tb, vb, a.v_sn, v0);
+            if (tb + 1 < nt) load(tb + 1, kb, a.k_sn, k1);
+        }
         uint4 qf[8];
         const float s2 = fabsf(a.s2);                   // a negative scale goes into the query's signs
         const uint32_t flip = a.s2 < 0.0f ? 0x80008000u : 0u;
@@ -127,52 +128,41 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
             ka[x] = (c32 >> 2) * kBlockBytes + (c32 & 3) * 256 + ((4 * x + hf) ^ (4 * (c32 & 3))) * 16;
             va[x] = hf * kBlockBytes + (c16 >> 2) * 256 + ((4 * x + vpiece) ^ (4 * (c16 >> 2))) * 16 + 8 * (c16 & 1);
         }
-        auto step = [&](int t, const char* kl, const char* vl, char* kn, char* vn) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();       // tile t is there, and every wave has left tile t - 1
-            if (t + 1 < nt) load(t + 1, kn, vn);
-            const int j0 = tile_begin(t), j1 = tile_end(t);
-            // nothing of the tile visible to this wave's rows
-            if (j0 > pw1 || (j0 >= a.sink && j1 - 1 <= pw0 - a.window)) return;
-            f32x16_v x[2];
+        auto products = [&](const char* kl, f32x16_v (&x)[2]) {
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[s][e] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)      // the two halves in turn: a product waits for the one before it on the same sums
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     const uint4 kf = *reinterpret_cast<const uint4*>(kl + ka[i >> 1] + 32 * (i & 1) + 8 * s * kBlockBytes);
                     x[s] = mfma32<DT>(kf, qf[i], x[s]);
                 }
-            // LDS reads run six products ahead
-            __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
-#pragma unroll
-            for (int i = 0; i < 10; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(kMfma, 6, 0);
+        };
+        // tile t's logits: those not visible masked, the reference raised where the maximum has outgrown it
+        auto settle = [&](int t, f32x16_v (&x)[2]) {
+            const int j0 = tile_begin(t), j1 = tile_end(t);
             // every row of the wave sees the whole tile, or masks
             const bool whole = j1 - j0 == kKeys && j1 - 1 <= pw0 && (j1 <= a.sink || j0 > pw1 - a.window);
             float mx = -INFINITY;
-            if (whole) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[s][e]);
-            } else {
+            if (!whole) {
+                // token j0 + 4 hf + i, i known at compile time: i <= hi, and i < sk or i > lo
+                const int at = j0 + 4 * hf, hi = min(p, j1 - 1) - at, sk = a.sink - at, lo = p - a.window - at;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int j = j0 + 32 * s + 4 * hf + (e & 3) + 8 * (e >> 2);
-                        const bool seen = j < j1 && j <= p && (j < a.sink || j > p - a.window);
+                        const int i = 32 * s + (e & 3) + 8 * (e >> 2);
+                        const bool seen = (i <= hi) & ((i < sk) | (i > lo));
                         x[s][e] = seen ? x[s][e] : -INFINITY;
-                        mx = fmaxf(mx, x[s][e]);
                     }
             }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[s][e]);
             mx = max_x32(mx) * s2;
             const bool grown = mx > m + kSlack;                 // m = -inf: the first visible tile
             if (__any(grown)) {
@@ -183,8 +173,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
 #pragma unroll
                 for (int d = 0; d < 4; ++d) o[d] *= al;
             }
+        };
+        auto weights = [&](const f32x16_v (&x)[2], uint4 (&pf)[4]) {
             const float ref = m == -INFINITY ? 0.0f : m;        // a row that has seen nothing yet: weights 0
-            uint4 pf[4];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -198,20 +189,56 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
                         u[e] = round_pair<DT>(y0, y1);
                     }
                     pf[2 * s + h8] = make_uint4(u[0], u[1], u[2], u[3]);
-                }
+                    asm("" : "+v"(l));                          // summed here, not where l is next read: the unrounded
+                }                                               // weights would stay in registers until then
+        };
+        auto values = [&](const char* vl, const uint4 (&pf)[4]) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {                       // 16 tokens each
+            for (int q = 0; q < 4; ++q)                         // 16 tokens each
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
                     const u32x2_v lo = read_transposed(vl + va[d] + 4 * q * kBlockBytes);
                     const u32x2_v hi = read_transposed(vl + va[d] + (4 * q + 2) * kBlockBytes);
                     o[d] = mfma32<DT>(make_uint4(lo.x, lo.y, hi.x, hi.y), pf[q], o[d]);
                 }
-            }
         };
-        for (int t = tb; t < nt; t += 2) {
-            step(t, k0, v0, k1, v1);
-            if (t + 1 < nt) step(t + 1, k1, v1, k0, v0);
+        auto arrive = [&] {   // what this step reads is there, and every wave has left what it loads over
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+        };
+        // tile t's weights and values, with tile t + 1's logits between them
+        auto step = [&](int t, f32x16_v (&x)[2], f32x16_v (&xn)[2], const char* kl, const char* vl, char* kn, char* vn) {
+            arrive();
+            if (t + 2 < nt) load(t + 2, kb, a.k_sn, kn);
+            load(t + 1, vb, a.v_sn, vn);
+            uint4 pf[4];
+            products(kl, xn);
+            weights(x, pf);
+            values(vl, pf);
+            settle(t + 1, xn);
+        };
+        auto last = [&](const f32x16_v (&x)[2], const char* vl) {
+            arrive();
+            uint4 pf[4];
+            weights(x, pf);
+            values(vl, pf);
+        };
+        if (tb < nt) {
+            f32x16_v xa[2], xb[2];
+            arrive();
+            products(k0, xa);
+            settle(tb, xa);
+            int t = tb;
+            for (; t + 2 < nt; t += 2) {
+                step(t, xa, xb, k1, v0, k0, v1);
+                step(t + 1, xb, xa, k0, v1, k1, v0);
+            }
+            if (t + 1 < nt) {
+                step(t, xa, xb, k1, v0, k0, v1);
+                last(xb, v1);
+            } else {
+                last(xa, v0);
+            }
         }
     }
     l += __shfl_xor(l, 32, 64);
