@@ -425,13 +425,15 @@ RefineArgs refine_args(const hill_desc* d, const Shape& s, const Layout& L, cons
 
 // Standalone selection: clear the counters, count the first digit, refine, emit.
 hill_status run_select(const hill_desc* d, const Shape& s, const Layout& L, const float* sacc, int32_t ksel,
-                       int32_t* idx, float* val, void* ws, hipStream_t st)
+                       int32_t* idx, float* val, void* ws, hipStream_t st, uint32_t* clear = nullptr,
+                       int64_t clear_words = 0)
 {
     const RefineArgs r = refine_args(d, s, L, sacc, ksel, ws);
     if (s.n <= kRowTopkTokens) {
-        HIP_TRY(launch_row_topk(r, s.B * s.R, idx, val, st));
+        HIP_TRY(launch_row_topk(r, s.B * s.R, idx, val, st, clear, clear_words));
         return HILL_OK;
     }
+    if (clear) HIP_TRY(launch_fill_zero(clear, clear_words, st));
     HIP_TRY(launch_fill_zero(at<uint32_t>(ws, L.zero), L.zero_words, st));
     HIP_TRY(launch_topk_hist(sacc, d->s_stride_b, d->s_stride_r, s.B, s.R, s.n, s.pin_lo, s.pin_hi,
                              at<uint32_t>(ws, L.hist1), st));
@@ -1133,8 +1135,7 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     EvictArgs a{};
     a.flags = at<uint32_t>(ws, flags);
     a.flag_words = evict_flag_words(chunks);
-    HIP_TRY(launch_fill_zero(a.flags, s.B * heads * a.flag_words, st));
-    HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st));
+    HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st, a.flags, s.B * heads * a.flag_words));
     a.idx = idx_out;
     a.B = s.B;
     a.R = s.R;

@@ -391,7 +391,9 @@ inline bool row_step(int B, int Hkv, int n, int k, bool kgather)
 constexpr int kRowTopkTokens = 32768;
 hipError_t launch_row_attend(const RefineArgs& r, const AttnArgs& at, int dtype, int32_t* idx, hipStream_t st,
                              Stamp ts = {});
-hipError_t launch_row_topk(const RefineArgs& r, int rows, int32_t* idx, float* val, hipStream_t st);
+// clear: words set to zero beside the selection, for the launch after it.
+hipError_t launch_row_topk(const RefineArgs& r, int rows, int32_t* idx, float* val, hipStream_t st,
+                           uint32_t* clear = nullptr, int64_t clear_words = 0);
 // One token's dense attention over a 16-bit or a packed cache (cache_attn.hip).
 struct CacheAttnArgs {
     const uint16_t* q;

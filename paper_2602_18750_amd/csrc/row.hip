@@ -281,11 +281,14 @@ __global__ __launch_bounds__(kRowThreads) void row_attend_kernel(RefineArgs r, A
 }
 
 template <int TPT>
-__global__ __launch_bounds__(kRowThreads) void row_topk_kernel(RefineArgs r, int32_t* idx, float* val)
+__global__ __launch_bounds__(kRowThreads) void row_topk_kernel(RefineArgs r, int32_t* idx, float* val,
+                                                                 uint32_t* clear, int64_t clear_words)
 {
     __shared__ RowLds rl;
     __shared__ __attribute__((aligned(16))) uint32_t bins[row_bin_words(8)];
     const int row = blockIdx.x, b = row / r.R;
+    for (int64_t i = (int64_t)row * kRowThreads + threadIdx.x; i < clear_words; i += (int64_t)gridDim.x * kRowThreads)
+        clear[i] = 0u;
     const float* srow = r.s + (int64_t)b * r.s_sb + (int64_t)(row % r.R) * r.s_sr;
     constexpr int GS = 4;
     uint32_t key[TPT];
@@ -350,10 +353,11 @@ hipError_t launch_row_attend(const RefineArgs& r, const AttnArgs& at, int dtype,
     return dtype == 1 ? launch_row_any<1>(r, at, idx, st, ts) : launch_row_any<0>(r, at, idx, st, ts);
 }
 
-hipError_t launch_row_topk(const RefineArgs& r, int rows, int32_t* idx, float* val, hipStream_t st)
+hipError_t launch_row_topk(const RefineArgs& r, int rows, int32_t* idx, float* val, hipStream_t st, uint32_t* clear,
+                           int64_t clear_words)
 {
     auto kernel = r.n <= 8 * kRowThreads ? row_topk_kernel<8> : r.n <= 16 * kRowThreads ? row_topk_kernel<16> : row_topk_kernel<32>;
-    hipLaunchKernelGGL(kernel, dim3(rows), dim3(kRowThreads), 0, st, r, idx, val);
+    hipLaunchKernelGGL(kernel, dim3(rows), dim3(kRowThreads), 0, st, r, idx, val, clear, clear_words);
     return hipGetLastError();
 }
 
