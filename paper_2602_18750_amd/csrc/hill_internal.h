@@ -471,15 +471,18 @@ struct PrefillArgs {
     float2* part_ml;          // [B,Hkv,t*G,nsplit]
     float s2;
 };
-// Rows per workgroup: 256 (eight waves) where that gives every CU one (of 256), since a workgroup's rows share the
-// keys and values it reads (16K x 16K tokens, window 4096: 986 -> 955 us); else 128.
-inline int prefill_rows(int64_t bh, int64_t rows) { return bh * ((rows + 255) / 256) >= 256 ? 256 : 128; }
-// Shares: where 128-row blocks leave a third of the two workgroups per CU without work, as many as fill them, of at
+// Rows per workgroup: 256 (eight waves) where their blocks need no shares (below), since a workgroup's rows share the keys
+// and values it reads; else 128.  128 -> 256 (us): 16K x 16K tokens, window 4096, GQA 32/8 986 -> 955; 4 x 509 new tokens
+// after 20K, GQA 28/4 (224 blocks of 256) 85.0 -> 77.9; 1400 after 8K (176) 129.9 -> 123.7; on the other side 1024 after 8K (128
+// blocks) 95.0 and, in four shares, 104.1.
+constexpr int kPrefillFull = 170;   // blocks: with more, one share each
+inline int prefill_rows(int64_t bh, int64_t rows) { return bh * ((rows + 255) / 256) > kPrefillFull ? 256 : 128; }
+// Shares: where 128-row blocks fill at most a third of the places (two workgroups per CU), as many as fill them, of at
 // least two 64-token tiles each.  One sequence, GQA 32/8, window 4096, one share -> several (us): 640 new tokens (160
 // blocks) 88.8 -> 69.3; on the other side 800 (200 blocks) 87.0 and 88.7, 1024 (256) 92.9 and 95.2.
 inline int prefill_splits(int64_t wgs, int64_t seen)
 {
-    if (wgs > 170) return 1;
+    if (wgs > kPrefillFull) return 1;
     const int64_t want = 512 / wgs, most = (seen + 127) / 128;
     return (int)(want < most ? want : most < 1 ? 1 : most);
 }
