@@ -318,7 +318,8 @@ HILL_API hill_status hill_step_sketch(const hill_desc* d, const void* q, const v
  *     j <= p  and  (j < n_sink  or  p - j < n_recent);
  * a query that sees nothing (an empty sequence, or n_sink = n_recent = 0) gets
  * zeros.  n_recent >= n_tokens attends to everything.  Tokens that no query of
- * the call sees are not read; whatever their rows hold has no effect.
+ * the call sees are not read; whatever their rows hold has no effect.  (A token that
+ * some queries of a prefill see has to hold finite values, for the others too.)
  *
  * lens: NULL, or device int32 [B], 4-byte aligned: the tokens of each sequence,
  * taken into [0, n_tokens] on the device (n_tokens is then the longest
@@ -356,7 +357,8 @@ HILL_API hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_
  *     code  = rint((x - zero) * (1 / scale)) in [0, 15], in fp32 (0 where scale is 0);
  * a code stands for fp16(code * scale + zero), rounded once.  Elements beyond
  * fp16's largest are taken as that.  160 bytes per token and KV head hold K and V,
- * instead of 512.
+ * instead of 512.  (Groups with elements near 65504 and far from it: the rounded scale
+ * can carry their largest code to infinity.)
  *
  * Layouts, all contiguous and 16-byte aligned: k_codes, v_codes [B, Hkv, cap, 64]
  * bytes (each little-endian 4-byte word holds elements 8w..8w+7: element 2i in bits
@@ -374,8 +376,8 @@ typedef struct hill_packed {
 
 /* Writes n_tokens rows of k and v (d's dtype and strides) per (b, g): row i of
  * sequence b becomes cache row at[b] + i (at: device int32 [B], 4-byte
- * aligned) or at0 + i (at NULL).  Rows that would land outside [0, cap) are not
- * written.  No score or q field of d is used. */
+ * aligned; rows that would land outside [0, cap) are not written) or at0 + i (at
+ * NULL; all of them inside).  No score or q field of d is used. */
 HILL_API hill_status hill_pack_kv(const hill_desc* d, const hill_packed* p, const void* k, const void* v, const int32_t* at,
                          int32_t at0, void* stream);
 

@@ -347,12 +347,9 @@ class _AttnCall:
     changes (and what lens, on the device, says).  Runs on the device and the stream that
     it was made for; its workspace and ``out`` are its own."""
 
-    def _marshal(self, fn, before, after, dev, stream, keep):
-        P = ctypes.c_void_p
-        self._fn, self._keep, self._dev = fn, keep, dev.index
-        self._before = before
-        self._after = tuple(P(x.data_ptr() if x is not None else None) if x is None or isinstance(x, torch.Tensor) else x
-                            for x in after)
+    def _marshal(self, fn, dev, keep, before, after):
+        self._fn, self._dev, self._keep, self._before = fn, dev.index, keep, before
+        self._after = tuple(ctypes.c_void_p(_ptr(x)) if x is None or isinstance(x, torch.Tensor) else x for x in after)
 
     def __call__(self, q_ptr: int):
         if torch._C._cuda_getDevice() != self._dev:
@@ -374,9 +371,8 @@ class WindowAttnCall(_AttnCall):
             self.out = _out(None, q)
             ref = ctypes.byref(self.desc)
             self.ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, 0), dev, ws)
-            self._marshal(lib.hill_window_attn, (ref,),
-                          (k, v, lens, self.out, self.ws, ctypes.c_size_t(ws_bytes), ctypes.c_void_p(_stream_ptr(None))),
-                          dev, stream, (k, v, lens))
+            self._marshal(lib.hill_window_attn, dev, (k, v, lens), (ref,),
+                          (k, v, lens, self.out, self.ws, ctypes.c_size_t(ws_bytes), ctypes.c_void_p(_stream_ptr(None))))
 
 
 class PackedAttnCall(_AttnCall):
@@ -391,6 +387,6 @@ class PackedAttnCall(_AttnCall):
             self.out = _out(None, q)
             ref = ctypes.byref(self.desc)
             self.ws, ws_bytes = _workspace(lib.hill_packed_workspace_bytes, (ref, k_sel, int(s is not None)), dev, ws)
-            self._marshal(lib.hill_packed_attn, (ref, ctypes.byref(cache.desc)),
+            self._marshal(lib.hill_packed_attn, dev, (cache, lens, idx, s), (ref, ctypes.byref(cache.desc)),
                           (lens, idx, ctypes.c_int32(k_sel), s, self.out, self.ws, ctypes.c_size_t(ws_bytes),
-                           ctypes.c_void_p(_stream_ptr(None))), dev, stream, (cache, lens, idx, s))
+                           ctypes.c_void_p(_stream_ptr(None))))

@@ -1,22 +1,34 @@
 // Attention of a chunk's tokens over the first tokens and a sliding window.
 //
 // The rows of a (sequence, KV head) are its T tokens times its G query heads,
-// token by token: a workgroup takes 128 of them (four waves of 32), so that a
-// group's heads share the keys and values they read and the rows of a workgroup lie
-// at few positions, whatever G.  It walks the first tokens and then the window
-// [first position - window + 1, last position] in tiles of 64, double-buffered in LDS by
-// direct loads, with running maxima and sums:
+// token by token: a workgroup takes 256 of them, or 128 (eight or four waves of
+// 32), so that a group's heads share the keys and values they read and the
+// rows of a workgroup lie at few positions, whatever G.  It walks the first
+// tokens and then the window [first position - window + 1, last position] in
+// tiles of 64, double-buffered in LDS by direct loads, with running maxima and
+// sums:
 //
 //   x^T = K Q^T on the matrix cores (tokens x rows): a lane holds one row's
 //   logits, the maximum needs one exchange between lane halves, and the weights
 //   are, rounded to 16 bits, the second product's operand as they lie;
 //   O^T += V^T w^T with V read from LDS transposed.
 //
-// The bound is the matrix cores, with the exponentials close behind.  Weights
-// are rounded to the cache's type (the output is rounded to it anyway); maxima,
-// sums and O are fp32.  The reference of the exponentials follows the running
-// maximum only when that has grown by more than 2^8: weights stay below 2^8 and
-// O is rescaled rarely.
+// Each tile's K Q^T products are formed among the exponentials of the tile
+// before it, whose weights then meet V: a wave's matrix and vector instructions
+// run side by side (at the size below 979 -> 950 us).  Weights are rounded to
+// the cache's type (the output is rounded to it anyway); maxima, sums and O are
+// fp32.  The reference of the exponentials follows the running maximum only
+// when that has grown by more than 2^8: weights stay below 2^8 and O is
+// rescaled rarely.
+//
+// Measured: 16K tokens, 32 / 8 heads, window 4096, 0.96 TFLOP: 935 to 950 us,
+// 1.02 PFLOP/s (large library products of the type reach 1.42 to 1.63).  The
+// matrix cores, LDS (each wave reads the whole tile for its 32 rows) and the
+// vector units (an exponential and about six more instructions per weight)
+// each need over half of that, and two waves per SIMD overlap them in part:
+// with K's reads from LDS left out 800 us, V's 905, the exponentials 872, all
+// three 684.  Sixty-four rows a wave halve the reads, but do not fit the
+// registers (1319 us with what that spills and moves).
 #include "mfma_device.h"
 
 namespace hill {
