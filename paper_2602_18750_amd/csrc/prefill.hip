@@ -25,10 +25,13 @@
 // 1.02 PFLOP/s (large library products of the type reach 1.42 to 1.63).  The
 // matrix cores, LDS (each wave reads the whole tile for its 32 rows) and the
 // vector units (an exponential and about six more instructions per weight)
-// each need over half of that, and two waves per SIMD overlap them in part:
-// with K's reads from LDS left out 800 us, V's 905, the exponentials 872, all
-// three 684.  Sixty-four rows a wave halve the reads, but do not fit the
-// registers (1319 us with what that spills and moves).
+// each need about half of that, two waves per SIMD overlap them in part (the
+// matrix cores are busy 0.94 of 1.77 million cycles), and the clock falls to
+// 1.5 to 1.9 GHz of 2.4 under the load: with K's reads from LDS left out 800 us,
+// V's 905, the exponentials 872, all three 684.  Sixty-four rows a wave halve
+// the reads, but do not fit the registers (1319 us with what that spills and
+// moves); the workgroup's halves in turn on the matrix cores and the vector
+// units, two barriers a tile, took the same cycles and time.
 #include "mfma_device.h"
 
 namespace hill {
