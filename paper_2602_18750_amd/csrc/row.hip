@@ -284,30 +284,79 @@ template <int TPT>
 __global__ __launch_bounds__(kRowThreads) void row_topk_kernel(RefineArgs r, int32_t* idx, float* val,
                                                                  uint32_t* clear, int64_t clear_words)
 {
+    constexpr int kCopies = 4;   // eight: 256 rows of 8K 7.8 -> 8.4 us, one of 32K the same
     __shared__ RowLds rl;
-    __shared__ __attribute__((aligned(16))) uint32_t bins[row_bin_words(8)];
+    __shared__ __attribute__((aligned(16))) uint32_t bins[row_bin_words(kCopies)];
     const int row = blockIdx.x, b = row / r.R;
     for (int64_t i = (int64_t)row * kRowThreads + threadIdx.x; i < clear_words; i += (int64_t)gridDim.x * kRowThreads)
         clear[i] = 0u;
     const float* srow = r.s + (int64_t)b * r.s_sb + (int64_t)(row % r.R) * r.s_sr;
-    constexpr int GS = 4;
-    uint32_t key[TPT];
-    bool ok[TPT], sel[TPT];
-    {
-        float sx[TPT];
-        row_load<TPT, GS>(srow, r.n, sx);
-        row_keys<TPT, GS>(sx, r.n, r.pin_lo, r.pin_hi, key, ok);
-    }
-    uint32_t p[TPT / GS];
-    row_select<TPT, GS, 8>(key, ok, (uint32_t)r.k, rl, bins, sel, p);
+    // One token per lane and element: 64 consecutive tokens are a mask, and the positions of the selected ones its bit
+    // counts.  Tokens past the row take key 0 like NaN, behind all others that have it: they are never among the first k.
+    const int lane = threadIdx.x & 63, t0 = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 * TPT;
+    const bool inside = t0 >= r.pin_lo && t0 + 64 * TPT <= r.pin_hi;   // neither pinned tokens nor the row's end
+    float sx[TPT];
+    if (inside) {
 #pragma unroll
-    for (int e = 0; e < TPT; ++e)
-        if (sel[e] && p[e / GS] < (uint32_t)r.k) {
-            const int j = row_token<TPT, GS>(e);
-            idx[(int64_t)row * r.k + p[e / GS]] = j;
-            if (val) val[(int64_t)row * r.k + p[e / GS]] = srow[j];   // read again: the keys fill the registers
-            ++p[e / GS];
+        for (int e = 0; e < TPT; ++e) sx[e] = srow[t0 + 64 * e + lane];
+    } else {
+#pragma unroll
+        for (int e = 0; e < TPT; ++e) sx[e] = srow[min(t0 + 64 * e + lane, r.n - 1)];
+    }
+    row_clear<kCopies>(bins);                             // while they are on their way
+    uint32_t key[TPT];
+    bool ok[TPT];
+    if (inside) {
+#pragma unroll
+        for (int e = 0; e < TPT; ++e) key[e] = order_key(sx[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < TPT; ++e) {
+            const int j = t0 + 64 * e + lane;
+            key[e] = j < r.n ? select_key(sx[e], j, r.pin_lo, r.pin_hi) : 0u;
         }
+    }
+#pragma unroll
+    for (int e = 0; e < TPT; ++e) ok[e] = inside || (uint32_t)(t0 + 64 * e + lane - r.pin_lo) < (uint32_t)(r.pin_hi - r.pin_lo);
+    // the pinned tokens, all of one key, are not counted: the threshold is that of the others
+    const uint32_t rest = (uint32_t)(r.k - (r.pin_lo == r.pin_hi ? r.n : r.pin_lo + r.n - r.pin_hi));
+    RowThreshold t{0xFFFFFFFFu, 0u, 0, true, {}};
+    if (rest > 0u) t = row_threshold<TPT, kCopies, true>(key, ok, rest, rl, bins, inside);
+    int32_t* to = idx + (int64_t)row * r.k;
+    float* vto = val ? val + (int64_t)row * r.k : nullptr;
+    const uint32_t least = t.prefix << t.shift;           // of the keys that are not below the threshold
+    auto write = [&](bool sel, int e, uint32_t& at) {
+        const uint64_t mask = __ballot(sel);
+        const uint32_t p = lanes_before(mask, at);
+        at += (uint32_t)__popcll(mask);
+        if (sel) {
+            const int j = t0 + 64 * e + lane;
+            to[p] = j;
+            if (vto) vto[p] = srow[j];   // read again: the keys fill the registers
+        }
+    };
+    uint32_t some = 0u;                                   // this wave's keys at or above the threshold
+#pragma unroll
+    for (int e = 0; e < TPT; ++e) some += (uint32_t)__popcll(__ballot(key[e] >= least));
+    uint32_t at = row_before(some, rl.wave[0]);
+    if (t.all_eq && t.prefix != 0u) {                     // else tokens past the row may be among the equal ones, as the last
+#pragma unroll
+        for (int e = 0; e < TPT; ++e) write(key[e] >= least, e, at);
+        return;
+    }
+    // the budget cuts through the keys equal to the threshold: the first t.need of them
+    uint32_t equal = 0u;
+#pragma unroll
+    for (int e = 0; e < TPT; ++e) equal += (uint32_t)__popcll(__ballot((key[e] >> t.shift) == t.prefix));
+    equal = row_before(equal, rl.wave[1]);
+    at -= equal - min(equal, t.need);
+#pragma unroll
+    for (int e = 0; e < TPT; ++e) {
+        const bool eq = (key[e] >> t.shift) == t.prefix;
+        const uint64_t mask = __ballot(eq);
+        write(eq ? lanes_before(mask, equal) < t.need : key[e] >= least, e, at);
+        equal += (uint32_t)__popcll(mask);
+    }
 }
 
 template <int DT, int GC, bool LG, bool TIER>

@@ -3,7 +3,8 @@
 // in bkp.hip).  Wave w holds 64 * TPT consecutive tokens in groups of GS per
 // lane: element e of lane l is token row_token<TPT, GS>(e), so that the lanes
 // of a load read consecutive groups (TPT consecutive tokens per thread read
-// each line TPT / 4 times: row_topk at 2 x 16K 19.8 us).
+// each line TPT / 4 times: row_topk at 2 x 16K 19.8 us, groups of four 11.1, and
+// with groups of one, whose positions are bit counts of masks, 8.5).
 #pragma once
 
 #include "hill_device.h"
@@ -114,24 +115,43 @@ struct RowBound {
     uint32_t b1, need1, in1;
 };
 
-// The keys of this thread's tokens to select, k of the row's n (1 <= k <= n):
-// sel[e] for token row_token(e); before[i]: tokens selected in the row before
-// this lane's group i.  ok[e]: the token exists (j < n).  bins: row_bin_words(COPIES)
-// words of LDS, 16-byte aligned, free again when it returns.  Every thread of
-// the workgroup calls it.
-template <int TPT, int GS, int COPIES>
-__device__ __forceinline__ RowBound row_select(const uint32_t (&key)[TPT], const bool (&ok)[TPT], uint32_t k, RowLds& L,
-                                               uint32_t* bins, bool (&sel)[TPT], uint32_t (&before)[TPT / GS])
+// The k-th largest key: keys above prefix at this shift are selected, and of
+// those equal to it `need`: all of them (all_eq) or the first in token order.
+struct RowThreshold {
+    uint32_t prefix, need;
+    int shift;
+    bool all_eq;
+    RowBound bound;
+};
+
+template <int COPIES>
+__device__ __forceinline__ void row_clear(uint32_t* bins)
+{
+#pragma unroll
+    for (int i = 0; i < kRowBins * COPIES / 4 / kRowThreads; ++i)
+        reinterpret_cast<uint4*>(bins)[i * kRowThreads + threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The threshold of the row's k largest (1 <= k <= n).  ok[e]: the token exists
+// (j < n); tokens that do not have key 0 and lie behind the others, so that they may
+// be counted too (ANY: where that saves tests; all: ok[e] for every e, of the whole wave).
+// bins: row_bin_words(COPIES) words of LDS, 16-byte aligned, cleared (row_clear); they
+// and L are free again when it returns.  Every thread of the workgroup calls it.
+template <int TPT, int COPIES, bool ANY = false>
+__device__ __forceinline__ RowThreshold row_threshold(const uint32_t (&key)[TPT], const bool (&ok)[TPT], uint32_t k,
+                                                      RowLds& L, uint32_t* bins, bool all = false)
 {
     const int tid = threadIdx.x;
     const uint32_t copy = tid & (COPIES - 1);
-#pragma unroll
-    for (int i = 0; i < kRowBins * COPIES / 4 / kRowThreads; ++i)
-        reinterpret_cast<uint4*>(bins)[i * kRowThreads + tid] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
+    if (ANY && all) {
 #pragma unroll
-    for (int e = 0; e < TPT; ++e)
-        if (ok[e]) atomicAdd(&bins[(key[e] >> 20) * COPIES + copy], 1u);
+        for (int e = 0; e < TPT; ++e) atomicAdd(&bins[(key[e] >> 20) * COPIES + copy], 1u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < TPT; ++e)
+            if (ok[e]) atomicAdd(&bins[(key[e] >> 20) * COPIES + copy], 1u);
+    }
     __syncthreads();
     row_find_bin<kRowBins, COPIES>(bins, L, k, L.wave[0]);
     const RowBound bound{L.res[0], L.res[1], L.res[2]};
@@ -148,7 +168,7 @@ __device__ __forceinline__ RowBound row_select(const uint32_t (&key)[TPT], const
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < TPT; ++e)
-            if (ok[e] && (key[e] >> shift) == prefix)
+            if ((ANY || ok[e]) && (key[e] >> shift) == prefix)
                 atomicAdd(&bins[((key[e] >> (shift - 10)) & 1023u) * COPIES + copy], 1u);
         __syncthreads();
         row_find_bin<kRowThreads, COPIES>(bins, L, need, L.wave[round & 1]);
@@ -157,8 +177,21 @@ __device__ __forceinline__ RowBound row_select(const uint32_t (&key)[TPT], const
         need = L.res[1];
         all_eq = need == L.res[2];
     }
-    // keys above the threshold's prefix, and of those equal to it all or, when
-    // the budget cuts through them, the first `need` in token order
+    return {prefix, need, shift, all_eq, bound};
+}
+
+// The keys of this thread's tokens to select, k of the row's n: sel[e] for
+// token row_token(e); before[i]: tokens selected in the row before this lane's
+// group i.  Else as row_threshold, but for the bins, which it clears itself.
+template <int TPT, int GS, int COPIES>
+__device__ __forceinline__ RowBound row_select(const uint32_t (&key)[TPT], const bool (&ok)[TPT], uint32_t k, RowLds& L,
+                                               uint32_t* bins, bool (&sel)[TPT], uint32_t (&before)[TPT / GS])
+{
+    row_clear<COPIES>(bins);
+    const RowThreshold t = row_threshold<TPT, COPIES>(key, ok, k, L, bins);
+    const uint32_t prefix = t.prefix, need = t.need;
+    const int shift = t.shift;
+    const bool all_eq = t.all_eq;
     constexpr int NG = TPT / GS;
     uint32_t cnt[NG];
     bool eq[TPT];
@@ -185,7 +218,24 @@ __device__ __forceinline__ RowBound row_select(const uint32_t (&key)[TPT], const
     }
     __syncthreads();   // earlier reads of the wave totals are done
     row_positions<NG>(cnt, L.wave[0], before);
-    return bound;
+    return t.bound;
+}
+
+// Sum over the row's waves before this one; v is uniform in a wave.  One
+// barrier; the totals stay in wave[], which must not be rewritten before the next.
+__device__ __forceinline__ uint32_t row_before(uint32_t v, uint32_t* wave)
+{
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (lane == 0) wave[w] = v;
+    __syncthreads();
+    const uint32_t t = lane < kRowWaves ? wave[lane] : 0u;
+    return (uint32_t)__builtin_amdgcn_readlane((int)(wave_incl_scan(t) - t), w);
+}
+
+// Lanes below this one whose bit is set, plus base.
+__device__ __forceinline__ uint32_t lanes_before(uint64_t mask, uint32_t base)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, base));
 }
 
 // This thread's floats of a row (16-byte aligned, its stride a multiple of 4

@@ -475,3 +475,22 @@ def test_evict_many_chunks_waits(held):
         H().hill_evict(si, keep, **args)
         for x, x0 in zip(bufs, before):
             assert torch.equal(x[:, :, :keep], x0[:, :, want[0, 0]]) and torch.equal(x[:, :, keep:], x0[:, :, keep:])
+
+
+# every token kept, or all but the lowest; numbers, NaN (below every number) and -inf at the threshold; rows that end with
+# a group of 64 tokens and within one; pins that leave the selection nothing to choose
+@pytest.mark.parametrize("n,k,sink,recent", [(64, 64, 0, 0), (256, 256, 0, 0), (300, 300, 0, 0), (8192, 8191, 0, 0),
+                                             (8193, 8193, 4, 64), (20032, 20032, 0, 0), (32768, 32768, 0, 0),
+                                             (1000, 68, 4, 64), (1000, 1000, 500, 500), (32768, 1028, 4, 1024),
+                                             (16384, 300, 0, 300), (1, 1, 0, 0)])
+@pytest.mark.parametrize("low", ["nan", "-inf", "number"])
+def test_selection_writes_its_own_rows(n, k, sink, recent, low):
+    g = torch.Generator().manual_seed(n + k)
+    s = torch.rand((2, 1, n), generator=g)
+    s[:, :, torch.randperm(n, generator=g)[:n // 2]] = float(low) if low != "number" else -1.0
+    si = H().new_importance(2, 1, n, DEV)
+    si.copy_(s)
+    guard = torch.full((64 + 2 * k + 40000,), -7, dtype=torch.int32, device=DEV)
+    idx = H().hill_topk(si, k, n_sink=sink, n_recent=recent, idx_out=guard[64:64 + 2 * k].view(2, 1, k))
+    assert torch.equal(idx.cpu().long(), R.kept(s, k, sink, recent))
+    assert (guard[:64] == -7).all() and (guard[64 + 2 * k:] == -7).all()
