@@ -9,8 +9,8 @@
 // handed out by its counter in ascending order, so every chunk waited for is held by a
 // workgroup that runs or has ended and sets its flag without waiting: each
 // wait ends.  Each kept row is read once and written once, past the caches; the
-// bound is a copy's: 16384 of 32768 rows of 8 KV heads, 134 MB, in 31.8 us (4.2 TB/s; a
-// 2 GiB copy reaches 5.0), 131072 of 4 x 65536 tokens, 1.07 GB, in 211 us (5.1 TB/s).
+// bound is a copy's: 16384 of 32768 rows of 8 KV heads, 134 MB, in 30.4 us (4.4 TB/s; a
+// 2 GiB copy reaches 5.0), 131072 of 4 x 65536 tokens, 1.07 GB, in 206 us (5.2 TB/s).
 #include "hill_device.h"
 #include "hill_internal.h"
 
@@ -91,9 +91,17 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a)
         for (int j = from + tid; j < to; j += 256) srow[j] = 0.0f;
     }
     if (!moves) return;
-    // chunks with a source among rows [d0, d0 + cnt)
-    for (int e = tid; e < c; e += 256) {
-        if (idx[e * kEvictChunk + kEvictChunk - 1] >= d0 && idx[e * kEvictChunk] < d0 + cnt)
+    // chunks with a source among rows [d0, d0 + cnt): each thread looks among a 256th of those before this one (the
+    // sources ascend), in one that has any for its first
+    const int per = (c + 255) / 256, e1 = min(per * (tid + 1), c);
+    int e = per * tid;
+    if (e < e1 && idx[e1 * kEvictChunk - 1] >= d0 && idx[e * kEvictChunk] < d0 + cnt) {
+        for (int hi = e1 - 1; e < hi;) {
+            const int mid = (e + hi) / 2;
+            if (idx[mid * kEvictChunk + kEvictChunk - 1] >= d0) hi = mid;
+            else e = mid + 1;
+        }
+        for (; e < e1 && idx[e * kEvictChunk] < d0 + cnt; ++e)
             for (int spin = 0; spin < kMaxSpins; ++spin) {
                 if (__hip_atomic_load(flags + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0u) break;
                 __builtin_amdgcn_s_sleep(1);
