@@ -386,7 +386,7 @@ inline bool row_step(int B, int Hkv, int n, int k, bool kgather)
 // 16K in 7.6 us instead of five launches of 18 and their boundaries.  Called as
 // a function with values, five launches -> one (us): one row of 4K 27.6 -> 8.3,
 // 16K 27.1 -> 9.3, 32K 27.0 -> 15.4; 32 rows of 32K 27.8 -> 17.3; 64 x 16K 28.0 ->
-// 10.6; 256 x 8K 39.5 -> 8.1, x 32K 109.7 -> 23.4; 512 x 4K 48.6 -> 9.8.  Longer rows
+// 10.6; 256 x 8K 39.5 -> 8.1, x 32K 109.7 -> 23.4; 512 x 4K 48.6 -> 8.3.  Longer rows
 // do not fit one workgroup's registers.
 constexpr int kRowTopkTokens = 32768;
 hipError_t launch_row_attend(const RefineArgs& r, const AttnArgs& at, int dtype, int32_t* idx, hipStream_t st,

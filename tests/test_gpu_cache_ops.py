@@ -482,7 +482,8 @@ def test_evict_many_chunks_waits(held):
 @pytest.mark.parametrize("n,k,sink,recent", [(64, 64, 0, 0), (256, 256, 0, 0), (300, 300, 0, 0), (8192, 8191, 0, 0),
                                              (8193, 8193, 4, 64), (20032, 20032, 0, 0), (32768, 32768, 0, 0),
                                              (1000, 68, 4, 64), (1000, 1000, 500, 500), (32768, 1028, 4, 1024),
-                                             (16384, 300, 0, 300), (1, 1, 0, 0)])
+                                             (16384, 300, 0, 300), (1, 1, 0, 0), (4096, 4095, 0, 0),
+                                             (4097, 2000, 0, 0), (24576, 24576, 0, 1), (24577, 12000, 3, 0)])
 @pytest.mark.parametrize("low", ["nan", "-inf", "number"])
 def test_selection_writes_its_own_rows(n, k, sink, recent, low):
     g = torch.Generator().manual_seed(n + k)
