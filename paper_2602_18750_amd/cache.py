@@ -93,8 +93,8 @@ def _count(name, x):
     return min(x, 2 ** 31 - 1)
 
 
-def _workspace(fn, args, dev, ws):
-    """ws, or one of the size that fn says (None for none)."""
+def _workspace(fn, args, like, ws):
+    """ws, or one of the size that fn says on like's device (None for none)."""
     if ws is not None:
         if not ws.is_contiguous():
             raise ValueError("ws must be contiguous")
@@ -103,7 +103,7 @@ def _workspace(fn, args, dev, ws):
     _check(fn(*args, ctypes.byref(need)))
     if need.value == 0:
         return None, 0
-    return torch.empty(need.value, dtype=torch.uint8, device=dev), need.value
+    return like.new_empty(need.value, dtype=torch.uint8), need.value
 
 
 def _kv_strides(k, v, B, D, dtype):
@@ -115,7 +115,7 @@ def _kv_strides(k, v, B, D, dtype):
 
 def _out(out, q):
     if out is None:
-        return torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        return q.new_empty(q.shape, dtype=torch.float32)
     if out.dtype != torch.float32 or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out must be a contiguous float32 tensor of q's shape")
     return out
@@ -142,7 +142,7 @@ def hill_window_attn(q, k, v, *, window, n_sink=0, n_tokens=None, lens=None, sm_
     with _on(dev, stream):
         out = _out(out, q)
         ref = ctypes.byref(d)
-        ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, 0), dev, ws)
+        ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, 0), q, ws)
         _check(lib.hill_window_attn(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lens), out.data_ptr(), _ptr(ws),
                                     ws_bytes, _stream_ptr(None)))
     return out
@@ -165,7 +165,7 @@ def hill_window_prefill(q, k, v, *, window, n_sink=0, n_tokens=None, lens=None, 
         o_st = _rows("out", out, 4, q.dtype)
         p = PrefillDesc(ctypes.sizeof(PrefillDesc), q.shape[2], q_st[2], *o_st)
         ref = ctypes.byref(d)
-        ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, q.shape[2]), dev, ws)
+        ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, q.shape[2]), q, ws)
         _check(lib.hill_window_prefill(ref, ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lens),
                                        out.data_ptr(), _ptr(ws), ws_bytes, _stream_ptr(None)))
     return out
@@ -283,7 +283,7 @@ def hill_packed_attn(q, cache: PackedCache, *, n_tokens=None, lens=None, n_sink=
     with _on(dev, stream):
         out = _out(out, q)
         ref = ctypes.byref(d)
-        ws, ws_bytes = _workspace(lib.hill_packed_workspace_bytes, (ref, k_sel, int(s is not None)), dev, ws)
+        ws, ws_bytes = _workspace(lib.hill_packed_workspace_bytes, (ref, k_sel, int(s is not None)), q, ws)
         _check(lib.hill_packed_attn(ref, ctypes.byref(cache.desc), q.data_ptr(), _ptr(lens), _ptr(idx), k_sel, _ptr(s),
                                     out.data_ptr(), _ptr(ws), ws_bytes, _stream_ptr(None)))
     return out
@@ -335,7 +335,7 @@ def hill_evict(s, k_keep, *, k=None, v=None, cache: Optional[PackedCache] = None
         else:
             _int32("idx_out", idx_out, (B, R, k_keep))
         ref = ctypes.byref(d)
-        ws, ws_bytes = _workspace(lib.hill_evict_workspace_bytes, (ref, k_keep), dev, ws)
+        ws, ws_bytes = _workspace(lib.hill_evict_workspace_bytes, (ref, k_keep), s, ws)
         _check(lib.hill_evict(ref, s.data_ptr(), k_keep, idx_out.data_ptr(), _ptr(k), _ptr(v),
                               None if cache is None else ctypes.byref(cache.desc), _ptr(pos), *p_st, _ptr(ws), ws_bytes,
                               _stream_ptr(None)))
@@ -370,7 +370,7 @@ class WindowAttnCall(_AttnCall):
         with _on(dev, stream):
             self.out = _out(None, q)
             ref = ctypes.byref(self.desc)
-            self.ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, 0), dev, ws)
+            self.ws, ws_bytes = _workspace(lib.hill_window_workspace_bytes, (ref, 0), q, ws)
             self._marshal(lib.hill_window_attn, dev, (k, v, lens), (ref,),
                           (k, v, lens, self.out, self.ws, ctypes.c_size_t(ws_bytes), ctypes.c_void_p(_stream_ptr(None))))
 
@@ -386,7 +386,7 @@ class PackedAttnCall(_AttnCall):
         with _on(dev, stream):
             self.out = _out(None, q)
             ref = ctypes.byref(self.desc)
-            self.ws, ws_bytes = _workspace(lib.hill_packed_workspace_bytes, (ref, k_sel, int(s is not None)), dev, ws)
+            self.ws, ws_bytes = _workspace(lib.hill_packed_workspace_bytes, (ref, k_sel, int(s is not None)), q, ws)
             self._marshal(lib.hill_packed_attn, dev, (cache, lens, idx, s), (ref, ctypes.byref(cache.desc)),
                           (lens, idx, ctypes.c_int32(k_sel), s, self.out, self.ws, ctypes.c_size_t(ws_bytes),
                            ctypes.c_void_p(_stream_ptr(None))))
