@@ -426,13 +426,15 @@ struct CacheAttnArgs {
 // loads) where they still make a workgroup per CU, else one.  A 32K layer with S, one position instead of four: 22.7 ->
 // 21.3 us; 4 x 131K keeps four.
 inline int score_per_thread(int64_t rows, int64_t seen) { return rows * ((seen + 1023) / 1024) >= 256 ? 4 : 1; }
-// Shares of `seen` visible positions: about two workgroups per CU (of 256) in
-// all, each of at least four 32-token tiles, one per wave.  Where the (sequence,
+// Shares of `seen` visible positions: one while three 32-token tiles a wave cost less than the launch that joins
+// (8 pairs, GQA 32/8, shares -> one, us in a graph: 150 positions 6.6 -> 5.6, 256 6.9 -> 5.7, 384 7.1 -> 6.9; on the other side 416 7.1
+// and 7.5, 512 7.2 and 7.8); else about two workgroups per CU (of 256) in all, each of at least four tiles, one per wave.  Where the (sequence,
 // KV head) pairs alone give every CU a workgroup, one share, and nothing to join: four waves' 16-bit
 // rows (64 KiB in flight) load a CU; packed rows (20 KiB) do not, and long ones are worth the join.  256 pairs, two
 // shares and one (us): 8 x 4K ragged, 16-bit, MHA 60.7 and 47.7; 32 x 16K packed, 8 KV heads 136 and 168.
 inline int cache_splits(int64_t wgs, int64_t seen, bool packed)
 {
+    if (seen <= 384) return 1;
     const int64_t alone = packed && seen >= 4096 ? 512 : 256;
     const int64_t want = wgs >= alone ? 1 : (512 + wgs / 2) / wgs, most = (seen + 127) / 128;
     const int64_t s = want < most ? want : most;
