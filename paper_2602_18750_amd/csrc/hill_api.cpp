@@ -715,7 +715,7 @@ PrefillLayout prefill_layout(const hill_desc* d, const Shape& s, int n_new)
     L.blocks = (rows + L.rows_per_wg - 1) / L.rows_per_wg;
     int64_t seen = (int64_t)d->n_sink + d->n_recent + L.rows_per_wg / s.G;   // tokens of a block's walk at most
     if (seen > s.n) seen = s.n;
-    L.nsplit = prefill_splits(bh * L.blocks, seen);
+    L.nsplit = prefill_splits(bh * L.blocks, bh * rows, seen);
     L.wgs = bh * L.blocks * L.nsplit;
     if (L.nsplit > 1) {
         L.part_ml = align256((size_t)bh * rows * L.nsplit * kHeadDim * sizeof(float));

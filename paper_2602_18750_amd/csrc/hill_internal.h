@@ -427,11 +427,12 @@ struct CacheAttnArgs {
 // 21.3 us; 4 x 131K keeps four.
 inline int score_per_thread(int64_t rows, int64_t seen) { return rows * ((seen + 1023) / 1024) >= 256 ? 4 : 1; }
 // Shares of `seen` visible positions: one while three 32-token tiles a wave cost less than the launch that joins
-// (8 pairs, GQA 32/8, shares -> one, us in a graph: 150 positions 6.6 -> 5.6, 256 6.9 -> 5.7, 384 7.1 -> 6.9; on the other side 416 7.1
-// and 7.5, 512 7.2 and 7.8); else about two workgroups per CU (of 256) in all, each of at least four tiles, one per wave.  Where the (sequence,
-// KV head) pairs alone give every CU a workgroup, one share, and nothing to join: four waves' 16-bit
-// rows (64 KiB in flight) load a CU; packed rows (20 KiB) do not, and long ones are worth the join.  256 pairs, two
-// shares and one (us): 8 x 4K ragged, 16-bit, MHA 60.7 and 47.7; 32 x 16K packed, 8 KV heads 136 and 168.
+// (8 pairs, GQA 32/8, shares -> one, us in a graph: 150 positions 6.6 -> 5.6, 256 6.9 -> 5.7, 384 7.1 -> 6.9; on the
+// other side 416 7.1 and 7.5, 512 7.2 and 7.8); else about two workgroups per CU (of 256) in all, each of at least four
+// tiles, one per wave.  Where the (sequence, KV head) pairs alone give every CU a workgroup, one share, and nothing to
+// join: four waves' 16-bit rows (64 KiB in flight) load a CU; packed rows (20 KiB) do not, and long ones are worth the
+// join.  256 pairs, two shares and one (us): 8 x 4K ragged, 16-bit, MHA 60.7 and 47.7; 32 x 16K packed, 8 KV heads 136
+// and 168.
 inline int cache_splits(int64_t wgs, int64_t seen, bool packed)
 {
     if (seen <= 384) return 1;
@@ -481,14 +482,26 @@ struct PrefillArgs {
 // blocks) 95.0 and, in four shares, 104.1.
 constexpr int kPrefillFull = 170;   // blocks: with more, one share each
 inline int prefill_rows(int64_t bh, int64_t rows) { return bh * ((rows + 255) / 256) > kPrefillFull ? 256 : 128; }
-// Shares: where 128-row blocks fill at most a third of the places (two workgroups per CU), as many as fill them, of at
-// least two 64-token tiles each.  One sequence, GQA 32/8, window 4096, one share -> several (us): 640 new tokens (160
-// blocks) 88.8 -> 69.3; on the other side 800 (200 blocks) 87.0 and 88.7, 1024 (256) 92.9 and 95.2.
-inline int prefill_splits(int64_t wgs, int64_t seen)
+// Shares, where 128-row blocks fill at most a third of the places (two workgroups per CU): as many as cost least, in
+// tiles of 64 tokens (1.0 us each; 1.4 with more than a workgroup per CU): a share's tiles and, with several, the join's
+// launch and the partial outputs that it reads (`rows` in all).  One share, these and as many as there are places (us in a
+// graph, 8 KV heads, 32 heads): 128 tokens, window 256 12.0, 11.8 (one), 14.1, window 1024 24.3, 19.0, 28.3; 1 token,
+// window 4096 68.6, 10.5, 10.5; 4 x 128 tokens, window 512 16.6, 16.7 (one), 26.0; 640 tokens after 8K, window 4096
+// 88.8, 67.4, 69.3; on the other side 800 (200 blocks) 87.0 and, in two, 88.7.
+inline int prefill_splits(int64_t wgs, int64_t rows, int64_t seen)
 {
     if (wgs > kPrefillFull) return 1;
-    const int64_t want = 512 / wgs, most = (seen + 127) / 128;
-    return (int)(want < most ? want : most < 1 ? 1 : most);
+    const int64_t tiles = (seen + 63) / 64, most = 512 / wgs < tiles ? 512 / wgs : tiles;
+    int best = 1;
+    double least = (double)tiles;
+    for (int64_t s = 2; s <= most; ++s) {
+        const double cost = (double)((tiles + s - 1) / s) * (wgs * s > 256 ? 1.4 : 1.0) + 1.2 + (double)(rows * s) / 3800.0;
+        if (cost < least) {
+            least = cost;
+            best = (int)s;
+        }
+    }
+    return best;
 }
 hipError_t launch_prefill(const PrefillArgs& a, int dtype, hipStream_t st);
 
