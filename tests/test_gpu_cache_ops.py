@@ -495,3 +495,28 @@ def test_selection_writes_its_own_rows(n, k, sink, recent, low):
     idx = H().hill_topk(si, k, n_sink=sink, n_recent=recent, idx_out=guard[64:64 + 2 * k].view(2, 1, k))
     assert torch.equal(idx.cpu().long(), R.kept(s, k, sink, recent))
     assert (guard[:64] == -7).all() and (guard[64 + 2 * k:] == -7).all()
+
+
+# two shares, some, dozens, hundreds; in the last sequence most of them are empty
+@pytest.mark.parametrize("n,B,Hq,Hkv", [(385, 2, 8, 2), (900, 2, 6, 3), (9001, 2, 4, 1), (70001, 2, 4, 1)])
+@pytest.mark.parametrize("held", ["16-bit", "packed"])
+def test_shares_of_one_token(n, B, Hq, Hkv, held):
+    q, k, v = draw((B, Hq, D), torch.float16, n), draw((B, Hkv, n, D), torch.float16, n + 1), draw((B, Hkv, n, D), torch.float16, n + 2)
+    lens = [n, 37]
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    if held == "packed":
+        cache = H().pack_kv(k.to(DEV), v.to(DEV), H().new_packed_cache(B, Hkv, n, DEV))
+        k, v = (x.cpu() for x in H().unpack_kv(cache))
+        out = H().hill_packed_attn(q.to(DEV), cache, lens=dl)
+    else:
+        out = H().hill_window_attn(q.to(DEV), k.to(DEV), v.to(DEV), window=n, lens=dl)
+    check_decode(out, q, k, v, lens, 0, n)
+
+
+@pytest.mark.parametrize("n,T,Hq,Hkv", [(700, 3, 8, 2), (1500, 33, 6, 3), (9001, 20, 4, 1), (40001, 2, 4, 1)])
+def test_shares_of_a_chunk(n, T, Hq, Hkv):
+    q, k, v = draw((2, Hq, T, D), torch.bfloat16, n), draw((2, Hkv, n, D), torch.bfloat16, n + 1), draw((2, Hkv, n, D), torch.bfloat16, n + 2)
+    lens = [n, 45]
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out = H().hill_window_prefill(q.to(DEV), k.to(DEV), v.to(DEV), window=n, n_sink=2, lens=dl)
+    check_prefill(out, q, k, v, lens, 2, n)
