@@ -226,8 +226,8 @@ def prepare(case, seed):
         st["cache"] = [_pack_rows(k) + _pack_rows(v) for k, v in kv]
         del st["kv"], kv
     elif c["kind"] == "write":
-        st["cache"] = [tuple(torch.zeros((b, hkv, n) + x, dtype=dt, device="cuda")
-                             for x, dt in (((64,), torch.uint8), ((4, 2), torch.float16)) * 2)]
+        st["cache"] = [(torch.zeros((b, hkv, n, 64), dtype=torch.uint8, device="cuda"),
+                        torch.zeros((b, hkv, n, 4, 2), dtype=torch.float16, device="cuda")) * 2]
     st["s"] = []
     for i in range(c["layers"] if c["kind"] == "evict" or c["score"] else 0):
         row = torch.zeros((b, r, (n + 3) // 4 * 4), device="cuda")[:, :, :n]
