@@ -238,7 +238,9 @@ def prepare(case, seed):
     if own:
         lib = _lib()
         st["ptrs"] = [[q[t, i].data_ptr() for i in range(c["layers"])] for t in range(q.shape[0])]
-        if "cache" in st:
+        if c["kind"] == "write":          # a cache of the package's own: it holds K and V side by side
+            st["caches"] = [lib.new_packed_cache(b, hkv, n, "cuda")]
+        elif "cache" in st:
             st["caches"] = [lib.PackedCache(*p) for p in st["cache"]]
         if c["kind"] == "window" and c["layers"] > 1:
             st["calls"] = [lib.WindowAttnCall(q[0, i, :, :, 0], k, v, window=c["window"], n_sink=c["sink"], lens=lens)
