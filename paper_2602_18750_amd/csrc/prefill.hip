@@ -100,8 +100,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
     float m = -INFINITY, l = 0.0f;
 
     if (pb >= 0) {
-        // tokens [0, ns) and [ws, pb]
-        const int ws = max(pa - a.window + 1, 0);
+        // tokens [0, ns) and [ws, pb], each of which some row of the block sees; without a window the sinks alone
+        const int ws = a.window > 0 ? max(pa - a.window + 1, 0) : pb + 1;
         const int ns = min(a.sink, ws);
         const int st = (ns + kKeys - 1) / kKeys, all = st + (pb + 1 - ws + kKeys - 1) / kKeys;
         const int per = (all + a.nsplit - 1) / a.nsplit, tb = split * per, nt = min(all, tb + per);   // this share's tiles
