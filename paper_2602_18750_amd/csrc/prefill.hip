@@ -18,8 +18,8 @@
 // run side by side (at the size below 979 -> 950 us).  Weights are rounded to
 // the cache's type (the output is rounded to it anyway); maxima, sums and O are
 // fp32.  The reference of the exponentials follows the running maximum only
-// when that has grown by more than 2^8: weights stay below 2^8 and O is
-// rescaled rarely.
+// when that has grown by more than 2^8 (fp16: 2^4): weights stay below that, and
+// O is rescaled rarely.
 //
 // Measured: 16K tokens, 32 / 8 heads, window 4096, 0.96 TFLOP: 935 to 950 us,
 // 1.02 PFLOP/s (large library products of the type reach 1.42 to 1.63).  The
@@ -45,7 +45,15 @@ constexpr int kKeys = 64;                       // tokens per tile
 // four rows by 64 bytes of V), and all of a lane's addresses are one of four and a constant.
 constexpr int kBlockBytes = 4 * kHeadDim * 2 + 16;
 constexpr int kTileBytes = kKeys / 4 * kBlockBytes;
-constexpr float kSlack = 8.0f;
+// How far (in the exponent of 2) a row's maximum may outgrow its reference before that follows, and the factor 2^shift
+// that the weights carry, in O and in their sum, until the division: bf16 reaches as far down as fp32, fp16 weights stay
+// below 2^15 and are whole (11 bits) down to 2^-25 of the reference, and multiples of 2^-35 below: behind a sink that takes
+// nearly all weight the others make the output.  (Slack and shift 8 and 0, 8 and 7, these, in us: 16K x 16K tokens, window
+// 4096, 968, 965, 978; 4 x 509 after 20K 72.8, 71.7, 73.8.)
+template <int DT>
+constexpr float kSlack = DT == 1 ? 8.0f : 4.0f;
+template <int DT>
+constexpr float kShift = DT == 1 ? 0.0f : 11.0f;
 
 __device__ __forceinline__ float max_x32(float v)
 {
@@ -179,7 +187,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[s][e]);
             mx = max_x32(mx) * s2;
-            const bool grown = mx > m + kSlack;                 // m = -inf: the first visible tile
+            const bool grown = mx > m + kSlack<DT>;                 // m = -inf: the first visible tile
             if (__any(grown)) {
                 const float m_new = grown ? mx : m;
                 const float al = grown ? exp2_ftz(m - m_new) : 1.0f;
@@ -190,7 +198,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_kernel(PrefillArgs a)
             }
         };
         auto weights = [&](const f32x16_v (&x)[2], uint4 (&pf)[4]) {
-            const float ref = m == -INFINITY ? 0.0f : m;        // a row that has seen nothing yet: weights 0
+            const float ref = m == -INFINITY ? 0.0f : m - kShift<DT>;   // a row that has seen nothing yet: weights 0
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
