@@ -364,7 +364,8 @@ HILL_API hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_
  * bytes (each little-endian 4-byte word holds elements 8w..8w+7: element 2i in bits
  * 4i..4i+3, element 2i+1 in bits 16+4i..19+4i); k_params, v_params
  * [B, Hkv, cap, 4] pairs of fp16 (scale, zero).  B, Hkv and the 16-bit dtype
- * are the descriptor's. */
+ * are the descriptor's.  Calls that write a cache (hill_pack_kv, hill_evict) want its
+ * four buffers disjoint. */
 typedef struct hill_packed {
     uint32_t struct_size;     /* sizeof(hill_packed) */
     int32_t cap;              /* rows per (b, g), >= 1 */

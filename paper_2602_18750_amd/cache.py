@@ -174,7 +174,8 @@ def hill_window_prefill(q, k, v, *, window, n_sink=0, n_tokens=None, lens=None, 
 class PackedCache:
     """K and V of one layer held in 4 bits (include/hill.h): codes [B, Hkv,
     cap, 64] uint8 and (scale, zero) of each group of 32 elements, [B, Hkv,
-    cap, 4, 2] fp16, both contiguous; 160 bytes per token and KV head."""
+    cap, 4, 2] fp16, both contiguous; 160 bytes per token and KV head.  A cache
+    that is written (pack_kv, hill_evict) has four buffers that do not overlap."""
 
     def __init__(self, k_codes, k_params, v_codes, v_params):
         B, Hkv, cap = k_codes.shape[:3]

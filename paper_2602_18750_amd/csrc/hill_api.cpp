@@ -635,6 +635,21 @@ hill_status check_packed(const hill_packed* p, int64_t rows)
     return HILL_OK;
 }
 
+// Calls that write a packed cache: no two of its buffers overlap (K's and V's rows are written side by side).
+hill_status check_packed_apart(const hill_packed* p, const Shape& s)
+{
+    const struct { const void* at; int row_bytes; const char* name; } buf[] = {
+        {p->k_codes, 64, "k_codes"}, {p->k_params, 16, "k_params"}, {p->v_codes, 64, "v_codes"}, {p->v_params, 16, "v_params"}};
+    const unsigned __int128 rows = (unsigned __int128)s.B * s.Hkv * p->cap;
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j) {
+            const uintptr_t lo = (uintptr_t)buf[i].at, hi = (uintptr_t)buf[j].at;
+            if (i != j && lo <= hi && hi - lo < rows * buf[i].row_bytes)
+                return fail(HILL_ERR_INVALID_ARG, "%s and %s of the packed cache overlap", buf[i].name, buf[j].name);
+        }
+    return HILL_OK;
+}
+
 // Launch grids hold 2^31 - 1 workgroups.
 hill_status check_grid(int64_t wgs)
 {
@@ -999,6 +1014,7 @@ hill_status hill_pack_kv(const hill_desc* d, const hill_packed* p, const void* k
     Shape s;
     HILL_TRY(check_desc(d, &s, false));
     HILL_TRY(check_packed(p, 1));
+    HILL_TRY(check_packed_apart(p, s));
     HILL_TRY(check_ptr(k, "k"));
     HILL_TRY(check_ptr(v, "v"));
     if ((uintptr_t)at & 3u) return fail(HILL_ERR_INVALID_ARG, "at is not 4-byte aligned");
@@ -1123,7 +1139,10 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
             (s.B > 1 && (d->k_stride_b < s.D || d->v_stride_b < s.D)))
             return fail(HILL_ERR_INVALID_ARG, "rows of k or v overlap");
     }
-    if (p) HILL_TRY(check_packed(p, s.n));
+    if (p) {
+        HILL_TRY(check_packed(p, s.n));
+        HILL_TRY(check_packed_apart(p, s));
+    }
     size_t flags;
     const size_t need = evict_bytes(s, k_keep, &flags);
     const int64_t chunks = evict_chunks(k_keep);
