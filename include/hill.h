@@ -339,7 +339,7 @@ HILL_API hill_status hill_window_attn(const hill_desc* d, const void* q, const v
  * already holds (a prefill, or one chunk of it).  q and out: [B, Hq, n_new, D] in
  * d's dtype, q with d's strides and q_stride_t between tokens, out with strides of its own, all
  * multiples of 8 elements (a [B, n_new, Hq, D] tensor has stride_t = Hq * D, stride_h = D);
- * both 16-byte aligned, out disjoint from the inputs.  Query i has position lens[b] - n_new + i;
+ * both 16-byte aligned, out's rows apart from one another and from the inputs.  Query i has position lens[b] - n_new + i;
  * where that is negative (a sequence shorter than the chunk, padded in front) its output is
  * zero.  The softmax weights and the output are rounded to d's dtype, sums are fp32. */
 typedef struct hill_prefill_desc {
@@ -384,7 +384,8 @@ HILL_API hill_status hill_pack_kv(const hill_desc* d, const hill_packed* p, cons
 
 /* Reads cache rows [token_begin, token_end) back as 16-bit rows: row
  * token_begin + i of (b, g) to row i of k and v (d's dtype and strides, n_tokens >=
- * token_end - token_begin rows); fp16 holds the values exactly, bf16 rounds them. */
+ * token_end - token_begin rows; no two rows overlap); fp16 holds the values exactly, bf16
+ * rounds them. */
 HILL_API hill_status hill_unpack_kv(const hill_desc* d, const hill_packed* p, int32_t token_begin, int32_t token_end, void* k,
                            void* v, void* stream);
 

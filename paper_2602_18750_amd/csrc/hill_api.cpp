@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstring>
 #include <string>
+#include <utility>
 
 #include "hill.h"
 #include "hill_internal.h"
@@ -635,6 +636,61 @@ hill_status check_packed(const hill_packed* p, int64_t rows)
     return HILL_OK;
 }
 
+// Rows of kHeadDim elements at i * st[0] + j * st[1] + l * st[2] for i, j, l below n[0], n[1], n[2]: the sizes and
+// strides (>= 0) of a strided 16-bit tensor that a call writes.
+struct RowSet {
+    int64_t n[3], st[3];
+};
+
+// Whether two of these rows meet when one of them lies `shift` elements further on (shift 0: two different ones).
+bool rows_meet(RowSet r, int64_t shift)
+{
+    for (int i = 0; i < 3; ++i)                          // the largest stride first
+        for (int j = i + 1; j < 3; ++j)
+            if (r.st[j] > r.st[i]) {
+                std::swap(r.st[i], r.st[j]);
+                std::swap(r.n[i], r.n[j]);
+            }
+    typedef __int128 wide;
+    const wide len = kHeadDim, reach2 = (wide)(r.n[2] - 1) * r.st[2], reach1 = reach2 + (wide)(r.n[1] - 1) * r.st[1];
+    // differences of a stride that may leave less than `limit` of `rest`: [lo, hi]
+    auto range = [](wide rest, int64_t st, int64_t n, wide limit, wide* lo, wide* hi) {
+        *lo = 1 - (wide)n;
+        *hi = (wide)n - 1;
+        if (st == 0) return;
+        const wide a = -(rest + limit - 1), b = -(rest - limit + 1);   // a <= d * st <= b
+        const wide l = a >= 0 ? (a + st - 1) / st : -(-a / st), h = b >= 0 ? b / st : -((-b + st - 1) / st);
+        if (l > *lo) *lo = l;
+        if (h < *hi) *hi = h;
+    };
+    wide lo0, hi0, lo1, hi1, lo2, hi2;
+    range(shift, r.st[0], r.n[0], reach1 + len, &lo0, &hi0);
+    if (shift == 0 && lo0 < 0) lo0 = 0;                  // a pair of rows counts once
+    for (wide a = lo0; a <= hi0; ++a) {
+        const wide rest0 = shift + a * r.st[0];
+        range(rest0, r.st[1], r.n[1], reach2 + len, &lo1, &hi1);
+        for (wide b = lo1; b <= hi1; ++b) {
+            const wide rest1 = rest0 + b * r.st[1];
+            range(rest1, r.st[2], r.n[2], len, &lo2, &hi2);
+            const bool same = shift == 0 && a == 0 && b == 0;          // then c = 0 is the row itself
+            if (lo2 <= hi2 && !(same && lo2 == 0 && hi2 == 0)) return true;
+        }
+    }
+    return false;
+}
+
+// K and V rows that a call writes: each set apart from itself and from the other (compared where both have the same strides).
+hill_status check_written_rows(const hill_desc* d, const Shape& s, int64_t rows, const void* k, const void* v, bool same_ok)
+{
+    const RowSet ks{{s.B, s.Hkv, rows}, {d->k_stride_b, d->k_stride_h, d->k_stride_n}};
+    const RowSet vs{{s.B, s.Hkv, rows}, {d->v_stride_b, d->v_stride_h, d->v_stride_n}};
+    if (rows_meet(ks, 0) || rows_meet(vs, 0)) return fail(HILL_ERR_INVALID_ARG, "rows of k or v overlap");
+    if (memcmp(ks.st, vs.st, sizeof(ks.st)) || (k == v && same_ok)) return HILL_OK;
+    const intptr_t apart = (intptr_t)v - (intptr_t)k;
+    if (apart == 0 || rows_meet(ks, apart / 2)) return fail(HILL_ERR_INVALID_ARG, "k and v overlap");
+    return HILL_OK;
+}
+
 // Calls that write a packed cache: no two of its buffers overlap (K's and V's rows are written side by side).
 hill_status check_packed_apart(const hill_packed* p, const Shape& s)
 {
@@ -962,6 +1018,8 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     if ((p->n_new > 1 && (p->q_stride_t < s.D || p->o_stride_t < s.D)) || (s.Hq > 1 && p->o_stride_h < s.D) ||
         (s.B > 1 && p->o_stride_b < s.D))
         return fail(HILL_ERR_INVALID_ARG, "q_stride_t or an out stride < head_dim");
+    if (rows_meet(RowSet{{s.B, s.Hq, p->n_new}, {p->o_stride_b, p->o_stride_h, p->o_stride_t}}, 0))
+        return fail(HILL_ERR_INVALID_ARG, "rows of out overlap");
     HILL_TRY(check_ptr(q, "q"));
     HILL_TRY(check_ptr(k, "k"));
     HILL_TRY(check_ptr(v, "v"));
@@ -1041,6 +1099,7 @@ hill_status hill_unpack_kv(const hill_desc* d, const hill_packed* p, int32_t tok
     if (token_end - token_begin > s.n)
         return fail(HILL_ERR_INVALID_ARG, "%d rows do not fit n_tokens %d", token_end - token_begin, s.n);
     if (token_begin == token_end) return HILL_OK;
+    HILL_TRY(check_written_rows(d, s, token_end - token_begin, k, v, false));
     PackArgs a = pack_args(d, s, p, k, v);
     a.at0 = token_begin;
     a.rows = token_end - token_begin;
@@ -1135,9 +1194,7 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     if (k) {
         HILL_TRY(check_ptr(k, "k"));
         HILL_TRY(check_ptr(v, "v"));
-        if ((s.Hkv > 1 && (d->k_stride_h < s.D || d->v_stride_h < s.D)) ||
-            (s.B > 1 && (d->k_stride_b < s.D || d->v_stride_b < s.D)))
-            return fail(HILL_ERR_INVALID_ARG, "rows of k or v overlap");
+        HILL_TRY(check_written_rows(d, s, s.n, k, v, true));   // (one buffer as both: its rows move alike)
     }
     if (p) {
         HILL_TRY(check_packed(p, s.n));

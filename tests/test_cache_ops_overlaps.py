@@ -1,10 +1,12 @@
 """Calls on the cache whose outputs would overlap are refused.  No GPU:
 validation fails before any pointer is used."""
 import ctypes
+import itertools
+import random
 
 import pytest
 
-from test_cache_ops_refusals import BIG, FAKE, H, INVALID, desc, packed  # noqa: F401  (H: a fixture)
+from test_cache_ops_refusals import BIG, FAKE, H, INVALID, WORKSPACE, desc, packed, prefill  # noqa: F401  (H: a fixture)
 
 
 def buffers(H, **at):
@@ -39,4 +41,85 @@ def test_buffers_that_only_touch_pass(H, at):
     d = desc(H, n=4, sink=0, recent=0)
     assert lib.hill_pack_kv(ctypes.byref(d), ctypes.byref(p), FAKE, FAKE, None, 7, None) == INVALID
     assert b"not inside" in lib.hill_last_error()
-    assert lib.hill_evict(ctypes.byref(d), FAKE, 2, FAKE, None, None, ctypes.byref(p), None, 0, 0, FAKE, 0, None) == 3
+    assert lib.hill_evict(ctypes.byref(d), FAKE, 2, FAKE, None, None, ctypes.byref(p), None, 0, 0, FAKE, 0, None) == WORKSPACE
+
+
+def layouts(seed):
+    """Sizes and strides of rows of 128 elements, [B, heads, tokens], nested in any order, and with gaps too small or none."""
+    rng = random.Random(seed)
+    for _ in range(400):
+        sizes = [rng.choice([1, 2, 3, 5]) for _ in range(3)]
+        strides, extent = [0, 0, 0], 128
+        for i in rng.sample(range(3), 3):
+            strides[i] = max(0, extent + 8 * rng.choice([0, 0, 1, 3, 16, -1, -16]))
+            extent = strides[i] * (sizes[i] - 1) + extent
+        if rng.random() < 0.3:
+            strides[rng.choice([0, 1])] = rng.choice([0, 8, 128, 136, 384])
+        strides[2] = max(strides[2], 128)
+        yield sizes, strides
+
+
+def starts(sizes, strides):
+    return sorted(sum(i * s for i, s in zip(at, strides)) for at in itertools.product(*map(range, sizes)))
+
+
+def meet(a, b):
+    """Whether a row that starts in a and one that starts in b have an element in common."""
+    return any(abs(x - y) < 128 for x in a for y in b)
+
+
+def test_rows_that_overlap_are_refused_and_no_others(H):
+    lib, seen = H.load_library(), [0, 0]
+    for (B, heads, n), (sb, sh, sn) in layouts(1):
+        at = starts((B, heads, n), (sb, sh, sn))
+        bad = any(y - x < 128 for x, y in zip(at, at[1:]))
+        seen[bad] += 1
+        d = desc(H, B=B, Hq=heads, Hkv=heads, n=n, sink=0, recent=0, k_stride_b=sb, k_stride_h=sh, k_stride_n=sn)
+        evict = lambda k, v: lib.hill_evict(ctypes.byref(d), FAKE, 1, FAKE, k, v, None, None, 0, 0, FAKE, 0, None)
+        assert evict(FAKE, FAKE + (1 << 30)) == (INVALID if bad else WORKSPACE), (B, heads, n, sb, sh, sn)
+        d.k_stride_b, d.k_stride_h, d.k_stride_n, d.v_stride_b, d.v_stride_h, d.v_stride_n = desc(H, B=B, Hkv=heads, n=n).k_stride_b, n * 128, 128, sb, sh, sn
+        assert evict(FAKE, FAKE + (1 << 30)) == (INVALID if bad else WORKSPACE), (B, heads, n, sb, sh, sn)
+        if sb >= 0 and B == 1:     # [1, heads, tokens] of a prefill's output: without a workspace it needs none, or too little
+            p = prefill(H, n_new=n, o_stride_b=sb, o_stride_h=max(sh, 128), o_stride_t=sn, q_stride_t=1024)
+            at = starts((1, heads, n), (0, max(sh, 128), sn))
+            if any(y - x < 128 for x, y in zip(at, at[1:])):
+                assert lib.hill_window_prefill(ctypes.byref(d), ctypes.byref(p), FAKE, FAKE, FAKE, None, FAKE, None, 0, None) == INVALID
+                assert b"rows of out overlap" in lib.hill_last_error()
+    assert min(seen) > 50
+
+
+def test_k_and_v_that_overlap_are_refused(H):
+    lib, rng, seen = H.load_library(), random.Random(2), [0, 0]
+    for (B, heads, n), (sb, sh, sn) in layouts(3):
+        at = starts((B, heads, n), (sb, sh, sn))
+        if any(y - x < 128 for x, y in zip(at, at[1:])):
+            continue
+        far = at[-1] // 8 + 16
+        shift = 8 * rng.choice([rng.randint(-far, far), 16, -16, 15, sn // 8, far, -far, 1 - far])
+        bad = meet([x + shift for x in at], at)
+        seen[bad] += 1
+        d = desc(H, B=B, Hq=heads, Hkv=heads, n=n, sink=0, recent=0, k_stride_b=sb, k_stride_h=sh, k_stride_n=sn,
+                 v_stride_b=sb, v_stride_h=sh, v_stride_n=sn)
+        k = FAKE + (1 << 24)
+        evict = lib.hill_evict(ctypes.byref(d), FAKE, 1, FAKE, k, k + 2 * shift, None, None, 0, 0, FAKE, 0, None)
+        assert evict == (INVALID if bad and shift else WORKSPACE), (B, heads, n, sb, sh, sn, shift)
+        p = buffers(H)
+        if bad:     # of the reader's outputs
+            assert lib.hill_unpack_kv(ctypes.byref(d), ctypes.byref(p), 2, 2 + n, k, k + 2 * shift, None) == INVALID
+            assert b"overlap" in lib.hill_last_error()
+    assert min(seen) > 30
+
+
+def test_outputs_with_overlapping_rows(H):
+    """The plain ways to make them: an expanded tensor, one buffer for two outputs, a window that slides by less than a row."""
+    lib, p = H.load_library(), buffers(H)
+    back = lambda k=FAKE, v=FAKE + 4096, **st: lib.hill_unpack_kv(
+        ctypes.byref(desc(H, n=8, **st)), ctypes.byref(p), 0, 8, k, v, None)
+    for bad in (dict(v=FAKE), dict(v=FAKE + 256), dict(k_stride_b=0), dict(v_stride_b=0), dict(k_stride_h=0), dict(v_stride_h=64)):
+        assert back(**bad) == INVALID, bad
+        assert b"overlap" in lib.hill_last_error()
+    d = desc(H)
+    for bad in (dict(o_stride_t=128), dict(o_stride_h=128, o_stride_t=1016), dict(o_stride_b=128), dict(o_stride_h=16 * 128 - 8, o_stride_t=128)):
+        q = prefill(H, **bad)
+        assert lib.hill_window_prefill(ctypes.byref(d), ctypes.byref(q), FAKE, FAKE, FAKE, None, FAKE, FAKE, BIG, None) == INVALID
+        assert b"rows of out overlap" in lib.hill_last_error(), bad
