@@ -80,8 +80,8 @@ def _int32(name, t, shape):
 
 def _tokens(n_tokens, most, what):
     n = most if n_tokens is None else int(n_tokens)
-    if n > most:
-        raise ValueError("n_tokens %d exceeds the %d of %s" % (n, most, what))
+    if not 0 <= n <= most:
+        raise ValueError("n_tokens %d is not among the %d of %s" % (n, most, what))
     return n
 
 
@@ -212,6 +212,8 @@ def pack_kv(k, v, cache: PackedCache, *, at=0, stream=None) -> PackedCache:
         raise ValueError("k has %d KV heads, the cache %d" % (Hkv, cache.n_kv_heads))
     if lens is not None:
         _int32("at", lens, (B,))
+    elif not 0 <= int(at) <= cache.cap - T:
+        raise ValueError("rows [%d, %d) are not inside the cache's %d" % (at, at + T, cache.cap))
     d = _desc(B, Hkv, Hkv, D, T, k.dtype, k_st=k_st, v_st=v_st)
     with _on(dev, stream):
         _check(lib.hill_pack_kv(ctypes.byref(d), ctypes.byref(cache.desc), k.data_ptr(), v.data_ptr(), _ptr(lens),
@@ -225,8 +227,8 @@ def unpack_kv(cache: PackedCache, *, token_begin=0, token_end=None, dtype=torch.
     lib = load_library()
     t1 = cache.cap if token_end is None else int(token_end)
     rows = t1 - int(token_begin)
-    if rows < 0:
-        raise ValueError("token range [%d, %d) is not one" % (token_begin, t1))
+    if not 0 <= int(token_begin) <= t1 <= cache.cap:
+        raise ValueError("rows [%d, %d) are not inside the cache's %d" % (token_begin, t1, cache.cap))
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
     dev = _device_of(("cache", cache.k_codes), ("k_out", k_out), ("v_out", v_out))

@@ -1,12 +1,14 @@
-"""Calls on the cache whose outputs would overlap are refused.  No GPU:
-validation fails before any pointer is used."""
+"""Calls on the cache whose outputs would overlap are refused, as are counts
+that the C structures' 32 bits would wrap around.  No GPU: validation fails
+before any pointer is used."""
 import ctypes
 import itertools
 import random
 
 import pytest
+import torch
 
-from test_cache_ops_refusals import BIG, FAKE, H, INVALID, WORKSPACE, desc, packed, prefill  # noqa: F401  (H: a fixture)
+from test_cache_ops_refusals import BIG, FAKE, H, INVALID, WORKSPACE, desc, meta, packed, prefill  # noqa: F401  (H: a fixture)
 
 
 def buffers(H, **at):
@@ -123,3 +125,41 @@ def test_outputs_with_overlapping_rows(H):
         q = prefill(H, **bad)
         assert lib.hill_window_prefill(ctypes.byref(d), ctypes.byref(q), FAKE, FAKE, FAKE, None, FAKE, FAKE, BIG, None) == INVALID
         assert b"rows of out overlap" in lib.hill_last_error(), bad
+
+
+@pytest.fixture
+def on_meta(H, monkeypatch):
+    """A packed cache of 2 x 2 x 50 rows without memory; calls that pass the binding's checks end in an error of their own."""
+    from paper_2602_18750_amd import cache as C
+    monkeypatch.setattr(C, "_device_of", lambda *named: torch.device("meta"))
+    monkeypatch.setattr(C, "_on", lambda *args: pytest.fail("accepted"))
+    monkeypatch.setattr(C, "_ptr", lambda t: pytest.fail("accepted"))
+    return H.new_packed_cache(2, 2, 50, "meta")
+
+
+WRAP = 1 << 32
+
+
+def test_counts_beyond_32_bits(H, on_meta):
+    cache, k = on_meta, meta(2, 2, 5, 128)
+    q, kv, s = meta(2, 8, 128), meta(2, 2, 50, 128), meta(2, 1, 52, dtype=torch.float32)
+    for call in (lambda x: H.pack_kv(k, k, cache, at=x), lambda x: H.unpack_kv(cache, token_begin=x, token_end=x + 5),
+                 lambda x: H.unpack_kv(cache, token_end=x + 5), lambda x: H.unpack_kv(cache, token_begin=x),
+                 lambda x: H.hill_window_attn(q, kv, kv, window=4, n_tokens=x + 5),
+                 lambda x: H.hill_window_prefill(q[:, :, None], kv, kv, window=4, n_tokens=x + 5),
+                 lambda x: H.hill_packed_attn(q, cache, n_tokens=x + 5), lambda x: H.PackedAttnCall(q, cache, n_tokens=x + 5),
+                 lambda x: H.hill_evict(s, x + 5, k=kv, v=kv), lambda x: H.hill_evict(s, 3, n_tokens=x + 5, k=kv, v=kv)):
+        for x in (WRAP, -WRAP, 7 * WRAP):
+            with pytest.raises(ValueError):
+                call(x)
+
+
+def test_ranges_of_the_writer_and_the_reader(H, on_meta):
+    cache = on_meta
+    rows = lambda n: meta(2, 2, n, 128)
+    for n, at in ((5, -1), (5, 46), (51, 0), (0, 51), (0, -1)):
+        with pytest.raises(ValueError):
+            H.pack_kv(rows(n), rows(n), cache, at=at)
+    for a, b in ((-1, 3), (4, 3), (0, 51), (51, 51), (50, 49)):
+        with pytest.raises(ValueError):
+            H.unpack_kv(cache, token_begin=a, token_end=b)
