@@ -214,6 +214,8 @@ def pack_kv(k, v, cache: PackedCache, *, at=0, stream=None) -> PackedCache:
         _int32("at", lens, (B,))
     elif not 0 <= int(at) <= cache.cap - T:
         raise ValueError("rows [%d, %d) are not inside the cache's %d" % (at, at + T, cache.cap))
+    if T == 0:
+        return cache
     d = _desc(B, Hkv, Hkv, D, T, k.dtype, k_st=k_st, v_st=v_st)
     with _on(dev, stream):
         _check(lib.hill_pack_kv(ctypes.byref(d), ctypes.byref(cache.desc), k.data_ptr(), v.data_ptr(), _ptr(lens),

@@ -163,3 +163,14 @@ def test_ranges_of_the_writer_and_the_reader(H, on_meta):
     for a, b in ((-1, 3), (4, 3), (0, 51), (51, 51), (50, 49)):
         with pytest.raises(ValueError):
             H.unpack_kv(cache, token_begin=a, token_end=b)
+
+
+def test_no_rows_are_written_and_read(H, on_meta, monkeypatch):
+    import contextlib
+    from paper_2602_18750_amd import cache as C
+    monkeypatch.setattr(C, "_on", lambda *args: contextlib.nullcontext())
+    cache, none = on_meta, meta(2, 2, 0, 128)
+    for at in (0, 17, 50):
+        assert H.pack_kv(none, none, cache, at=at) is cache
+        assert H.unpack_kv(cache, token_begin=at, token_end=at)[0].shape == (2, 2, 0, 128)
+    assert H.pack_kv(none, none, cache, at=meta(2, dtype=torch.int32)) is cache
