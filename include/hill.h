@@ -353,12 +353,12 @@ HILL_API hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_
                                 const void* v, const int32_t* lens, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* Cache held in 4 bits.  A row of 128 elements is four groups of 32, each with
- *     scale = fp16((max - min) * (1/15 in fp32)),  zero = fp16(min);
+ *     scale = fp16((max - min) * (1/15 in fp32)),  zero = fp16(min),
+ *             the next smaller scale where fp16(15 * scale + zero) is infinite;
  *     code  = rint((x - zero) * (1 / scale)) in [0, 15], in fp32 (0 where scale is 0);
  * a code stands for fp16(code * scale + zero), rounded once.  Elements beyond
- * fp16's largest are taken as that.  160 bytes per token and KV head hold K and V,
- * instead of 512.  (Groups with elements near 65504 and far from it: the rounded scale
- * can carry their largest code to infinity.)
+ * fp16's largest are taken as that: finite rows come back finite.  160 bytes per token
+ * and KV head hold K and V, instead of 512.
  *
  * Layouts, all contiguous and 16-byte aligned: k_codes, v_codes [B, Hkv, cap, 64]
  * bytes (each little-endian 4-byte word holds elements 8w..8w+7: element 2i in bits

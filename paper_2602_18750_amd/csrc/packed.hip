@@ -60,7 +60,11 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
             hi = max4(hi);
             float step = (hi - lo) * (1.0f / 15.0f);
             asm("" : "+v"(step));   // an fp32 value before it becomes fp16: not one rounding of the product
-            const _Float16 scale = (_Float16)step, zero = (_Float16)lo;
+            _Float16 scale = (_Float16)step;
+            const _Float16 zero = (_Float16)lo;
+            // rounded up, a scale can carry the largest code past fp16's range: then the one below it
+            if (__builtin_elementwise_fma((_Float16)15.0f, scale, zero) == (_Float16)INFINITY)
+                scale = __builtin_bit_cast(_Float16, (uint16_t)(__builtin_bit_cast(uint16_t, scale) - 1));
             const float inv = (float)scale > 0.0f ? 1.0f / (float)scale : 0.0f;
             uint32_t word = 0u;
 #pragma unroll
