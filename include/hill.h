@@ -419,7 +419,15 @@ HILL_API hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, 
  * were.  The order of tokens stays, so the first n_sink and the last tokens are
  * where selections, windows and later evictions look for them.  A key sketch or
  * pool state of the cache is not moved: rewrite it (hill_sketch_keys), or clear it;
- * a streamed selection goes on with a zeroed state. */
+ * a streamed selection goes on with a zeroed state.
+ *
+ * Every sequence is n_tokens long here (n_recent pins the last of those): a batch whose
+ * lengths differ is evicted in calls of its own per length.
+ *
+ * Calls that run at the same time need workspaces of their own, here above all: one that
+ * finds its workspace's flags used by another leaves rows where they were.  The uint32 at
+ * byte hill_evict_workspace_bytes - 256 of the workspace says so once the call's work is
+ * done: 0, or how many parts of the move were left out. */
 HILL_API hill_status hill_evict_workspace_bytes(const hill_desc* d, int32_t k_keep, size_t* bytes);
 HILL_API hill_status hill_evict(const hill_desc* d, float* s, int32_t k_keep, int32_t* idx_out, void* k, void* v,
                        const hill_packed* p, int32_t* pos, int64_t pos_stride_b, int64_t pos_stride_r, void* ws,

@@ -17,6 +17,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhill.so")
 # the benchmark's roofline calibration read, a library of its own (not libhill's ABI)
 CALIB_LIB = os.path.join(PKG, "libhill_calib.so")
+# the move of hill_evict by itself, for the test of what it does when a wait finds no end
+MOVE_LIB = os.path.join(PKG, "libhill_move.so")
 # the same library with its host layer (hill_api.cpp: validation, workspace
 # layouts, launch set-up) built with AddressSanitizer and UBSan, for CPU runs
 # of the error paths with the sanitizer runtime preloaded; device code as in LIB
@@ -30,6 +32,7 @@ RESOURCES = os.path.join(BUILD_DIR, "kernel_resources.txt")
 SOURCES = ["hill_api.cpp", "score.hip", "update.hip", "sketch.hip", "topk.hip", "row.hip", "attn.hip", "bkp.hip", "noalloc.hip", "tier.hip",
            "cache_attn.hip", "packed.hip", "prefill.hip", "evict.hip"]
 CALIB_SOURCES = ["calib.hip"]
+MOVE_SOURCES = ["evict_move.cpp"]   # with evict.hip's object
 ARCH = os.environ.get("HILL_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -113,11 +116,12 @@ def build_host_sanitized(verbose: bool = False) -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
-    srcs = SOURCES + CALIB_SOURCES
+    srcs = SOURCES + CALIB_SOURCES + MOVE_SOURCES
     with ThreadPoolExecutor(max_workers=len(srcs)) as ex:
         objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
     _link([objs[s] for s in SOURCES], LIB, verbose)
     _link([objs[s] for s in CALIB_SOURCES], CALIB_LIB, verbose)
+    _link([objs[s] for s in MOVE_SOURCES + ["evict.hip"]], MOVE_LIB, verbose)
     _resource_report()
     return LIB
 

@@ -299,7 +299,8 @@ def hill_evict(s, k_keep, *, k=None, v=None, cache: Optional[PackedCache] = None
     """Makes the cache k_keep tokens long: the k_keep largest S of each row
     stay (the first n_sink and last n_recent always), in order and in place, in
     k and v or in ``cache``, in s (zero behind them) and in pos (int32, s's
-    shape and strides).  Returns their former indices [B, R, k_keep] int32."""
+    shape and strides).  Returns their former indices [B, R, k_keep] int32.  Calls that
+    run at the same time need a ``ws`` each (the call's own, if none is given)."""
     lib = load_library()
     k_keep = int(k_keep)
     if (k is None) != (v is None) or (k is not None and cache is not None):

@@ -8,7 +8,7 @@
 // chunks before it (a source never lies before its destination), and a group's chunks are
 // handed out by its counter in ascending order, so every chunk waited for is held by a
 // workgroup that runs or has ended and sets its flag without waiting: each
-// wait ends.  Each kept row is read once and written once, past the caches; the
+// wait ends (kMaxSpins).  Each kept row is read once and written once, past the caches; the
 // bound is a copy's: 16384 of 32768 rows of 8 KV heads, 134 MB, in 30.4 us (4.4 TB/s; a
 // 2 GiB copy reaches 5.0), 131072 of 4 x 65536 tokens, 1.07 GB, in 206 us (5.2 TB/s).
 #include "hill_device.h"
@@ -21,7 +21,8 @@ namespace {
 constexpr int kLoads = kEvictChunk / 16;   // 16-bit rows per lane group (16 lanes a row)
 
 // A wait lasts a few microseconds; the limit (tens of milliseconds) ends it where
-// two calls share one workspace at a time, against the contract.
+// two calls share one workspace at a time, against the contract.  The workgroup then
+// leaves its rows as they are and says so in the status word.
 constexpr int kMaxSpins = 1 << 16;
 
 // Stores wait for the flag seen before them, loads for the flag set after them.
@@ -31,16 +32,22 @@ template <bool ROWS, bool PACKED>
 __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a)
 {
     __shared__ int32_t src[kEvictChunk];
-    __shared__ int ticket;
+    __shared__ int ticket, late;
     const int tid = threadIdx.x;
     const int groups = a.B * a.heads;
     const int bg = blockIdx.x % groups;
     uint32_t* flags = a.flags + (int64_t)bg * a.flag_words;
-    if (tid == 0) ticket = (int)atomicAdd(flags, 1u);
+    if (tid == 0) {
+        ticket = (int)atomicAdd(flags, 1u);
+        late = 0;
+    }
     ++flags;
     __syncthreads();
     const int c = ticket;
-    if ((unsigned)c >= (unsigned)a.chunks) return;           // only where two calls share a workspace
+    if ((unsigned)c >= (unsigned)a.chunks) {                 // only where two calls share a workspace
+        if (tid == 0) atomicAdd(a.status, 1u);
+        return;
+    }
     const int b = bg / a.heads, g = bg % a.heads;
     const int r = a.R > 1 ? g : 0;
     const int32_t* idx = a.idx + ((int64_t)b * a.R + r) * a.keep;
@@ -101,14 +108,21 @@ __global__ __launch_bounds__(256) void evict_kernel(EvictArgs a)
             if (idx[mid * kEvictChunk + kEvictChunk - 1] >= d0) hi = mid;
             else e = mid + 1;
         }
-        for (; e < e1 && idx[e * kEvictChunk] < d0 + cnt; ++e)
-            for (int spin = 0; spin < kMaxSpins; ++spin) {
-                if (__hip_atomic_load(flags + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0u) break;
+        for (int spins = kMaxSpins; e < e1 && idx[e * kEvictChunk] < d0 + cnt; ++e) {
+            while (__hip_atomic_load(flags + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0u && --spins > 0)
                 __builtin_amdgcn_s_sleep(1);
+            if (spins <= 0) {
+                late = 1;
+                break;
             }
+        }
     }
     asm volatile("" ::: "memory");
     __syncthreads();
+    if (late) {
+        if (tid == 0) atomicAdd(a.status, 1u);
+        return;
+    }
     if constexpr (ROWS) {
         uint16_t* k = a.k + (int64_t)b * a.k_sb + (int64_t)g * a.k_sh + l16 * 8;
         uint16_t* v = a.v + (int64_t)b * a.v_sb + (int64_t)g * a.v_sh + l16 * 8;

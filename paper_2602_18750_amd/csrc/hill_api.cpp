@@ -821,7 +821,7 @@ PackArgs pack_args(const hill_desc* d, const Shape& s, const hill_packed* p, voi
     return a;
 }
 
-// The selection's regions without those of the scores, then the eviction's flags.
+// The selection's regions without those of the scores, then the eviction's flags and 256 bytes that begin with its status.
 Shape evict_shape(Shape s)
 {
     s.mode = HILL_SCORE_RAW;
@@ -834,7 +834,7 @@ int64_t evict_chunks(int k_keep) { return (k_keep + kEvictChunk - 1) / kEvictChu
 size_t evict_bytes(const Shape& s, int k_keep, size_t* flags)
 {
     *flags = layout_for(evict_shape(s), k_keep).end_topk;
-    return *flags + align256((size_t)s.B * s.Hkv * evict_flag_words(evict_chunks(k_keep)) * sizeof(uint32_t));
+    return *flags + align256((size_t)s.B * s.Hkv * evict_flag_words(evict_chunks(k_keep)) * sizeof(uint32_t)) + 256;
 }
 
 }  // namespace
@@ -1211,7 +1211,8 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     EvictArgs a{};
     a.flags = at<uint32_t>(ws, flags);
     a.flag_words = evict_flag_words(chunks);
-    HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st, a.flags, s.B * heads * a.flag_words));
+    a.status = at<uint32_t>(ws, need - 256);
+    HILL_TRY(run_select(d, s, L, s_acc, k_keep, idx_out, nullptr, ws, st, a.flags, a.status + 1 - a.flags));
     a.idx = idx_out;
     a.B = s.B;
     a.R = s.R;

@@ -523,6 +523,7 @@ struct EvictArgs {
     uint32_t* flags;          // [B * heads, flag_words]: a group's ticket counter, then its chunks whose sources have
                               //   been read; zeroed
     int64_t flag_words;
+    uint32_t* status;         // zeroed: workgroups that left their rows as they were
     int heads;                // row groups per sequence that move: Hkv, or R without K and V
     int chunks;
 };
