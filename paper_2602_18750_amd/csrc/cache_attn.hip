@@ -331,13 +331,13 @@ __global__ __launch_bounds__(256, KT == kRowsPacked ? 4 : 3) void cache_attn_ker
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, p[e]);
         const float m_new = fmaxf(m, max_x16_x32(mx) * s2);
         if (__any(m_new > m)) {
-            const float al = exp2_ftz(m - m_new);
+            const float al = m_new > m ? exp2_ftz(m - m_new) : 1.0f;
             l *= al;
 #pragma unroll
             for (int d = 0; d < 8; ++d) o[d] *= al;
         }
         m = m_new;
-        const float ref = m - kWeightShift<DT>;
+        const float ref = m == -INFINITY ? 0.0f : m - kWeightShift<DT>;   // logits below fp32's range alone so far: weights 0
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             p[e] = exp2_ftz(__builtin_fmaf(p[e], s2, -ref));
@@ -444,8 +444,8 @@ __device__ __forceinline__ void add_weights(const CacheAttnArgs& a, int64_t bloc
             const float2 v = red[tid * tph + u];
             L += v.y > 0.0f ? v.y * exp2_ftz(v.x - M) : 0.0f;
         }
-        // the shares' l carry the weights' factor
-        stat[tid] = make_float2(M - kWeightShift<0>, 1.0f / L);
+        // the shares' l carry the weights' factor; nothing but logits below fp32's range: weights 0
+        stat[tid] = L > 0.0f ? make_float2(M - kWeightShift<0>, 1.0f / L) : make_float2(0.0f, 0.0f);
     }
     __syncthreads();
     if (i >= vis.nv) return;
