@@ -1204,7 +1204,7 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     const size_t need = evict_bytes(s, k_keep, &flags);
     const int64_t chunks = evict_chunks(k_keep);
     const int heads = k || p ? s.Hkv : s.R;
-    HILL_TRY(check_grid(s.B * heads * chunks));
+    HILL_TRY(check_grid((int64_t)s.B * heads * chunks));
     HILL_TRY(check_ws(ws, ws_bytes, need));
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Layout L = layout_for(evict_shape(s), k_keep);

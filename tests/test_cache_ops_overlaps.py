@@ -1,5 +1,5 @@
 """Calls on the cache whose outputs would overlap are refused, as are counts
-that the C structures' 32 bits would wrap around.  No GPU: validation fails
+that 32 bits would wrap around.  No GPU: validation fails
 before any pointer is used."""
 import ctypes
 import itertools
@@ -8,7 +8,7 @@ import random
 import pytest
 import torch
 
-from test_cache_ops_refusals import BIG, FAKE, H, INVALID, WORKSPACE, desc, meta, packed, prefill  # noqa: F401  (H: a fixture)
+from test_cache_ops_refusals import BIG, FAKE, H, INVALID, UNSUPPORTED, WORKSPACE, desc, meta, packed, prefill  # noqa: F401  (H: a fixture)
 
 
 def buffers(H, **at):
@@ -174,3 +174,13 @@ def test_no_rows_are_written_and_read(H, on_meta, monkeypatch):
         assert H.pack_kv(none, none, cache, at=at) is cache
         assert H.unpack_kv(cache, token_begin=at, token_end=at)[0].shape == (2, 2, 0, 128)
     assert H.pack_kv(none, none, cache, at=meta(2, dtype=torch.int32)) is cache
+
+
+@pytest.mark.parametrize("B,heads", [(1 << 30, 4), (1 << 29, 8), (1 << 28, 16), ((1 << 31) - 1, 2), ((1 << 31) - 1, 256)])
+def test_an_evictions_grid_in_64_bits(H, B, heads):
+    """B * heads is a multiple of 2^32, or wraps to something small."""
+    d = desc(H, B=B, Hq=heads, Hkv=heads, n=8, sink=0, recent=0, gran=1)
+    ask = lambda: H.load_library().hill_evict(ctypes.byref(d), FAKE, 1, FAKE, None, None, None, None, 0, 0, FAKE,
+                                                   (1 << 64) - 1, None)
+    assert ask() == UNSUPPORTED
+    assert b"workgroups" in H.load_library().hill_last_error()
