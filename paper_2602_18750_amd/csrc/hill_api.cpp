@@ -706,10 +706,11 @@ hill_status check_packed_apart(const hill_packed* p, const Shape& s)
     return HILL_OK;
 }
 
-// Launch grids hold 2^31 - 1 workgroups.
-hill_status check_grid(int64_t wgs)
+// A launch holds fewer than 2^32 threads.
+hill_status check_grid(int64_t wgs, int threads)
 {
-    if (wgs > INT32_MAX) return fail(HILL_ERR_UNSUPPORTED, "batch and heads need %lld workgroups", (long long)wgs);
+    if (wgs > (int64_t)(UINT32_MAX / (unsigned)threads))
+        return fail(HILL_ERR_UNSUPPORTED, "batch and heads need %lld workgroups of %d threads", (long long)wgs, threads);
     return HILL_OK;
 }
 
@@ -986,7 +987,7 @@ hill_status hill_window_attn(const hill_desc* d, const void* q, const void* k, c
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
     const CacheLayout L = cache_layout(d, s, 0, false, false);
-    HILL_TRY(check_grid(L.wgs + 4 * (int64_t)s.B * s.Hq));
+    HILL_TRY(check_grid(L.wgs, 256));                     // (several shares: few sequences, and a small launch joins them)
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
     a.k = static_cast<const uint16_t*>(k);
@@ -1026,7 +1027,7 @@ hill_status hill_window_prefill(const hill_desc* d, const hill_prefill_desc* p, 
     HILL_TRY(check_lens(lens));
     HILL_TRY(check_ptr(out, "out"));
     const PrefillLayout L = prefill_layout(d, s, p->n_new);
-    HILL_TRY(check_grid(L.wgs > (int64_t)s.B * s.Hq * p->n_new ? L.wgs : (int64_t)s.B * s.Hq * p->n_new));
+    HILL_TRY(check_grid(L.wgs, 2 * L.rows_per_wg));       // (several shares: few rows, and a small launch joins them)
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     PrefillArgs a{};
     a.q = static_cast<const uint16_t*>(q);
@@ -1137,7 +1138,8 @@ hill_status hill_packed_attn(const hill_desc* d, const hill_packed* p, const voi
     HILL_TRY(check_ptr(out, "out"));
     const CacheLayout L = cache_layout(d, s, idx ? k_sel : 0, s_acc != nullptr, true);
     const int s_per = score_per_thread((int64_t)s.B * s.R, L.ld), s_chunks = (int)((L.ld + 256 * s_per - 1) / (256 * s_per));
-    HILL_TRY(check_grid(L.wgs + 4 * (int64_t)s.B * s.Hq + (int64_t)s.B * s.R * s_chunks));
+    HILL_TRY(check_grid(L.wgs, 256));
+    HILL_TRY(check_grid((L.nsplit > 1 ? 4 * (int64_t)s.B * s.Hq : 0) + (s_acc ? (int64_t)s.B * s.R * s_chunks : 0), 256));
     HILL_TRY(check_ws(ws, ws_bytes, L.end));
     CacheAttnArgs a = cache_args(d, s, L, q, lens, out, ws);
     uint8_t *kc, *vc;
@@ -1204,7 +1206,8 @@ hill_status hill_evict(const hill_desc* d, float* s_acc, int32_t k_keep, int32_t
     const size_t need = evict_bytes(s, k_keep, &flags);
     const int64_t chunks = evict_chunks(k_keep);
     const int heads = k || p ? s.Hkv : s.R;
-    HILL_TRY(check_grid((int64_t)s.B * heads * chunks));
+    HILL_TRY(check_grid((int64_t)s.B * heads * chunks, 256));
+    if (s.n <= kRowTopkTokens) HILL_TRY(check_grid((int64_t)s.B * s.R, 1024));
     HILL_TRY(check_ws(ws, ws_bytes, need));
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Layout L = layout_for(evict_shape(s), k_keep);

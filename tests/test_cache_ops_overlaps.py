@@ -1,5 +1,5 @@
 """Calls on the cache whose outputs would overlap are refused, as are counts
-that 32 bits would wrap around.  No GPU: validation fails
+that 32 bits would wrap around and launches of 2^32 threads.  No GPU: validation fails
 before any pointer is used."""
 import ctypes
 import itertools
@@ -184,3 +184,28 @@ def test_an_evictions_grid_in_64_bits(H, B, heads):
                                                    (1 << 64) - 1, None)
     assert ask() == UNSUPPORTED
     assert b"workgroups" in H.load_library().hill_last_error()
+
+
+def test_launches_hold_fewer_than_2_to_the_32_threads(H):
+    """The last batch that fits passes on to the workspace's check (where it needs one), the next is refused."""
+    lib, p = H.load_library(), packed(H, cap=8)
+    small = dict(n=8, sink=0, recent=8)
+
+    def evict(B, heads, keep, gran, n=8):
+        d = desc(H, B=B, Hq=heads, Hkv=heads, n=n, sink=0, recent=0, gran=gran)
+        return lib.hill_evict(ctypes.byref(d), FAKE, keep, FAKE, None, None, None, None, 0, 0, FAKE, 0, None)
+
+    def score(B, heads):
+        d = desc(H, B=B, Hq=heads, Hkv=heads, **small)
+        return lib.hill_packed_attn(ctypes.byref(d), ctypes.byref(p), FAKE, None, None, 0, FAKE, FAKE, FAKE, 0, None)
+
+    assert evict((1 << 20) - 1, 4, 8, 1) == WORKSPACE and evict(1 << 20, 4, 8, 1) == UNSUPPORTED      # the selection's
+    assert evict(1 << 22, 1, 8, 0) == UNSUPPORTED
+    assert evict(511, 1, 1 << 21, 0, n=1 << 21) == WORKSPACE                                          # the move's
+    assert evict(512, 1, 1 << 21, 0, n=1 << 21) == UNSUPPORTED
+    assert score((1 << 21) - 1, 8) == WORKSPACE and score(1 << 21, 8) == UNSUPPORTED
+    d = desc(H, B=1 << 21, Hq=8, Hkv=8, **small)
+    assert lib.hill_window_attn(ctypes.byref(d), FAKE, FAKE, FAKE, None, FAKE, FAKE, BIG, None) == UNSUPPORTED
+    assert lib.hill_packed_attn(ctypes.byref(d), ctypes.byref(p), FAKE, None, None, 0, None, FAKE, FAKE, BIG, None) == UNSUPPORTED
+    q = prefill(H, n_new=8, o_stride_b=8 * 8 * 128)
+    assert lib.hill_window_prefill(ctypes.byref(d), ctypes.byref(q), FAKE, FAKE, FAKE, None, FAKE, FAKE, BIG, None) == UNSUPPORTED
