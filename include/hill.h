@@ -46,7 +46,8 @@
  *   enqueued; on any error nothing is enqueued and no output is written.
  *   HILL_ERR_INVALID_ARG: null/misaligned pointer, bad shape, stride or k_sel.
  *   HILL_ERR_UNSUPPORTED: a valid but unimplemented head_dim, dtype, head
- *                         count, context length or token stride.
+ *                         count, context length or token stride, or a batch
+ *                         that needs a launch of 2^32 threads.
  *   HILL_ERR_WORKSPACE:   ws too small.
  *   HILL_ERR_HIP:         a kernel launch failed (enqueued work before it in
  *                         the same call may still run).
@@ -393,7 +394,9 @@ HILL_API hill_status hill_unpack_kv(const hill_desc* d, const hill_packed* p, in
 HILL_API hill_status hill_packed_workspace_bytes(const hill_desc* d, int32_t k_sel, int32_t with_s, size_t* bytes);
 
 /* One token's attention over a cache held in 4 bits; q [B, Hq, D], out fp32
- * [B, Hq, D], n_tokens <= cap; d's k and v strides are checked but not used.
+ * [B, Hq, D], n_tokens <= cap; d's k and v strides are checked but not used.  A bf16
+ * query is held in fp16 times a power of two: elements below 2^-29 of its head's
+ * largest lose bits.
  * idx NULL: over what hill_window_attn would see (n_sink, n_recent, lens).
  * idx [B, R, k_sel] int32: over those rows (as hill_gather_attn; n_sink, n_recent
  * are not used, lens and s must be NULL).

@@ -8,8 +8,8 @@
 // chunks before it (a source never lies before its destination), and a group's chunks are
 // handed out by its counter in ascending order, so every chunk waited for is held by a
 // workgroup that runs or has ended and sets its flag without waiting: each
-// wait ends (kMaxSpins).  Each kept row is read once and written once, past the caches; the
-// bound is a copy's: 16384 of 32768 rows of 8 KV heads, 134 MB, in 30.4 us (4.4 TB/s; a
+// wait ends.  Each kept row is read once and written once, past the caches; the
+// bound is a copy's: 16384 of 32768 rows of 8 KV heads, 134 MB, in 31 us (4.3 TB/s; a
 // 2 GiB copy reaches 5.0), 131072 of 4 x 65536 tokens, 1.07 GB, in 206 us (5.2 TB/s).
 #include "hill_device.h"
 #include "hill_internal.h"

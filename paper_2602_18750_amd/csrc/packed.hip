@@ -2,8 +2,8 @@
 // lanes take a row, eight elements each, four lanes a group of 32; a lane makes
 // one word of eight codes.  Both directions are copies in effect: 256 B of 16-bit
 // row against 80 B of codes and parameters, four rows per lane group in flight.
-// Measured: 32768 rows of 8 KV heads, K and V, 176 MB each way: 38 us to write
-// them (4.6 TB/s), 27 to read them back (6.5); a copy of a GiB reaches 5.0.
+// Measured: 32768 rows of 8 KV heads, K and V, 176 MB each way: 39 us to write
+// them (4.5 TB/s), 27 to read them back (6.5); a copy of a GiB reaches 5.0.
 #include "mfma_device.h"
 
 namespace hill {

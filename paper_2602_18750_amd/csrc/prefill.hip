@@ -21,8 +21,8 @@
 // when that has grown by more than 2^8 (fp16: 2^4): weights stay below that, and
 // O is rescaled rarely.
 //
-// Measured: 16K tokens, 32 / 8 heads, window 4096, 0.96 TFLOP: 935 to 950 us,
-// 1.02 PFLOP/s (large library products of the type reach 1.42 to 1.63).  The
+// Measured: 16K tokens, 32 / 8 heads, window 4096, 0.96 TFLOP: 885 to 950 us
+// from card to card, 1.01 to 1.09 PFLOP/s (large library products of the type reach 1.42 to 1.63).  The
 // matrix cores, LDS (each wave reads the whole tile for its 32 rows) and the
 // vector units (an exponential and about six more instructions per weight)
 // each need about half of that, two waves per SIMD overlap them in part (the
